@@ -249,6 +249,78 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
                       void *cuda_stream);
 
 /*
+ * Scored steps: kvf_fold_step and kvf_attend for models whose scores are more than scale * (q . k).  With s that
+ * product, token i of the chunk, query head h and cache row r,
+ *     s <- softcap * tanh(s / softcap)              (softcap > 0)
+ *     s <- s - slopes[h] * |pos0 + i - r|           (slopes given: a bias that falls with the distance; a row's position is its index)
+ *     r is seen if first[i] <= r < end[i]           (either given; else first = 0 and end = the token's own row + 1, or, for
+ *                                                    kvf_attend_scored, every row the cache holds)
+ * so that documents packed one after the other see only themselves (first), and a prompt sees itself both ways (end).  Entries of
+ * first and end out of range mean the nearest row there is.  A token whose range is empty gets zeros and a
+ * log-sum-exp of -inf.  (The paper's models have plain scores; a chunk of the fold under a cap, a bias or such a mask is
+ * the same step, Section 2.)
+ *   softcap  >= 0 and finite, 0 = none       slopes   device, [n_q_heads] fp32, or NULL
+ *   first    device, [n_tokens] int32, or NULL       end      device, [n_tokens] int32, or NULL
+ * The device arrays are read in stream order and may be changed behind the call.  Everything else - rows appended whatever the ranges
+ * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend.  Not under a sink + window mask
+ * and not on quantised storage (KVF_ERR_UNSUPPORTED).  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
+ * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
+ * A cap rounds each score to about 2^-20 of the largest it can become.
+ */
+typedef struct kvf_scores {
+    double softcap;
+    const float *slopes;
+    const int32_t *first;
+    const int32_t *end;
+} kvf_scores;
+kvf_status kvf_fold_step_scored(kvf_cache *c, const void *q, const void *k_new, const void *v_new, int32_t n_tokens, int64_t pos0,
+                                const kvf_scores *scores, void *out, float *lse, void *cuda_stream);
+kvf_status kvf_attend_scored(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos0, const kvf_scores *scores, void *out, float *lse,
+                             void *cuda_stream);
+
+/* The queries of a chunk rotated as the step rotates them (the same bits): q, q_rot device, [n_tokens][H][d] dtype, contiguous,
+ * 16-byte aligned; q_rot may be q.  n_tokens <= max_chunk.  One kernel on cuda_stream; the cache is not touched. */
+kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos0, void *q_rot, void *cuda_stream);
+
+/*
+ * The attention weight that a chunk's queries give the rows of the cache, per KV head g and row r:
+ *     mass_out[g][r] = decay * mass_in[g][r] + sum over tokens i and query heads h of g of exp(s_ihr - lse[i][h]),
+ * over the rows that token i sees (the same s and the same rows as in the step that left lse).  (The paper's Discussion prunes a
+ * folded cache by attention weight and gives no scheme; this is what such schemes add up, and kvf_cache_evict goes by.)
+ *   q_rot      device, [n_tokens][H][d] dtype: the queries AFTER rotation (kvf_rotate_queries)
+ *   appended   1: the queries are those of the last n_tokens rows of the cache, call after kvf_fold_step; token i sees rows up to
+ *              its own; those rows start from zero, whatever mass_in holds there.  0: they see every row (kvf_attend)
+ *   pos0       position of token 0; matters with slopes only
+ *   scores     as in the step, or NULL
+ *   lse        device, [n_tokens][H] fp32, natural log, from the step (-inf: the row saw nothing and gives nothing)
+ *   mass_in    device, [n_kv_heads][in_stride] fp32, or NULL (zeros; also where decay is 0: then it is not read)
+ *   mass_out   device, [n_kv_heads][out_stride] fp32: rows [0, kvf_cache_len) of each head are written, the others left alone.
+ *              May be mass_in (with the same stride), must not overlap it otherwise.  Strides >= kvf_cache_len
+ * Sums are fp32 and their order depends on shapes alone.  Not on quantised storage and not under a sink + window mask
+ * (KVF_ERR_UNSUPPORTED).  Asynchronous on cuda_stream, uses no workspace but the status word.
+ */
+kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int32_t appended, int64_t pos0, const kvf_scores *scores,
+                          const float *lse, const float *mass_in, int64_t in_stride, float decay, float *mass_out, int64_t out_stride,
+                          void *cuda_stream);
+
+/*
+ * Eviction by accumulated weight: `budget` rows of every KV head of `from` become rows 0 .. budget - 1 of `to`, in order: the
+ * first n_sink, the last n_recent, and of those between the ones with the largest mass, each KV head for itself; of equal
+ * masses the lower rows stay; NaN counts as less than any number.  kvf_cache_len(to) becomes budget; `from` is not changed.
+ * (The Discussion of the paper, attention-based pruning.)  Kept rows keep their rotation; the next step on `to` appends behind
+ * them and takes its position from pos0, which the caller passes on (the positions do not shrink with the rows).
+ *   from, to    two caches of the same heads, head_dim, dtype and storage (bf16, fp32, int8, int4), contiguous or paged in any
+ *               combination, of which no byte is shared; paged caches of one pool with different pages
+ *   mass        device, [n_kv_heads][mass_stride] fp32, mass_stride >= kvf_cache_len(from)
+ *   budget      n_sink + n_recent <= budget <= kvf_cache_len(from), and <= the capacity of `to` (KVF_ERR_CAPACITY)
+ *   mass_out    device, [n_kv_heads][out_stride] fp32, out_stride >= budget, not over mass: the kept rows' mass; or NULL
+ *   kept        device, [n_kv_heads][budget] int32: the kept rows' numbers in `from`, ascending
+ * Two kernels on cuda_stream, no workspace.
+ */
+kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *mass, int64_t mass_stride, int64_t n_sink, int64_t n_recent,
+                           int64_t budget, float *mass_out, int64_t out_stride, int32_t *kept, void *cuda_stream);
+
+/*
  * Merges n_parts attention results over disjoint sets of rows into the result over their union:
  *     lse = log sum_r exp(lse_r),   out = sum_r exp(lse_r - lse) * out_r     (parts in index order).
  * parts_out: device, [n_parts][n_rows][head_dim], elements of `dtype` (KVF_BF16 or KVF_F32: what the

@@ -31,6 +31,7 @@ EXPORTS = [
     "kvf_batch_status_word", "kvf_batch_launch_count", "kvf_batch_destroy", "kvf_cache_set_window",
     "kvf_batch_fold_step_ragged", "kvf_cache_k_scales", "kvf_cache_v_scales", "kvf_cache_sm_clock",
     "kvf_cache_host_flush", "kvf_batch_fold_step_varlen", "kvf_cache_flush",
+    "kvf_fold_step_scored", "kvf_attend_scored", "kvf_rotate_queries", "kvf_cache_mass", "kvf_cache_evict",
 ]
 
 
@@ -41,6 +42,10 @@ class kvf_config(ctypes.Structure):
         ("flags", ctypes.c_uint32), ("rope_base", ctypes.c_double), ("softmax_scale", ctypes.c_double),
         ("inv_freq", ctypes.POINTER(ctypes.c_double)),
     ]
+
+
+class kvf_scores(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_double), ("slopes", ctypes.c_void_p), ("first", ctypes.c_void_p), ("end", ctypes.c_void_p)]
 
 
 class KvfError(RuntimeError):
@@ -91,6 +96,17 @@ def load() -> ctypes.CDLL:
     lib.kvf_cache_len.restype = i64
     lib.kvf_cache_reset.argtypes = [vp]
     lib.kvf_cache_reset.restype = ctypes.c_int
+    scp = ctypes.POINTER(kvf_scores)
+    lib.kvf_fold_step_scored.argtypes = [vp, vp, vp, vp, i32, i64, scp, vp, vp, vp]
+    lib.kvf_fold_step_scored.restype = ctypes.c_int
+    lib.kvf_attend_scored.argtypes = [vp, vp, i32, i64, scp, vp, vp, vp]
+    lib.kvf_attend_scored.restype = ctypes.c_int
+    lib.kvf_rotate_queries.argtypes = [vp, vp, i32, i64, vp, vp]
+    lib.kvf_rotate_queries.restype = ctypes.c_int
+    lib.kvf_cache_mass.argtypes = [vp, vp, i32, i32, i64, scp, vp, vp, i64, ctypes.c_float, vp, i64, vp]
+    lib.kvf_cache_mass.restype = ctypes.c_int
+    lib.kvf_cache_evict.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, i64, vp, vp]
+    lib.kvf_cache_evict.restype = ctypes.c_int
     lib.kvf_attend.argtypes = [vp, vp, i32, i64, vp, vp, vp]
     lib.kvf_attend.restype = ctypes.c_int
     lib.kvf_merge_partials.argtypes = [i32, i64, i32, ctypes.c_int, vp, vp, vp, vp, vp]
@@ -185,6 +201,17 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
+def _scores(softcap, slopes, first, end, heads: int, n: int) -> Optional[kvf_scores]:
+    """kvf_scores of a step's keywords, or None where none was given (a plain step)."""
+    if not softcap and slopes is None and first is None and end is None:
+        return None
+    if slopes is not None:
+        assert slopes.is_cuda and slopes.is_contiguous() and slopes.dtype is torch.float32 and slopes.numel() == heads
+    for t in (first, end):
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype is torch.int32 and t.numel() == n)
+    return kvf_scores(softcap, *(None if t is None else t.data_ptr() for t in (slopes, first, end)))
+
+
 class Cache:
     """One layer's accumulated K/V on the current CUDA device (kvf_cache_* calls)."""
 
@@ -234,8 +261,11 @@ class Cache:
 
     def fold_step(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                   pos0: Optional[int] = None, out: Optional[torch.Tensor] = None,
-                  lse: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """kvf_fold_step on device tensors; returns the chunk's attention output."""
+                  lse: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, softcap: float = 0.0,
+                  slopes: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None,
+                  end: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """kvf_fold_step on device tensors; returns the chunk's attention output.  With any of softcap, slopes ([H] fp32),
+        first, end ([n] int32) kvf_fold_step_scored."""
         # (a step of a toy model is a few microseconds on the GPU: the call does no more than it needs)
         lib, h, dtype = _lib or load(), self._h, self.torch_dtype
         assert q.is_cuda and q.is_contiguous() and q.dtype is dtype
@@ -244,6 +274,14 @@ class Cache:
         n = q.shape[0]
         if out is None:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        if scores is not None:
+            rc = lib.kvf_fold_step_scored(h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), n,
+                                          lib.kvf_cache_len(h) if pos0 is None else int(pos0), ctypes.byref(scores), out.data_ptr(),
+                                          None if lse is None else lse.data_ptr(), _stream_ptr(stream))
+            if rc != KVF_OK:
+                raise KvfError(rc, "kvf_fold_step_scored")
+            return out
         rc = lib.kvf_fold_step(h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), n,
                                lib.kvf_cache_len(h) if pos0 is None else int(pos0), out.data_ptr(),
                                None if lse is None else lse.data_ptr(), _stream_ptr(stream))
@@ -252,17 +290,81 @@ class Cache:
         return out
 
     def attend(self, q: torch.Tensor, pos0: Optional[int] = None, out: Optional[torch.Tensor] = None,
-               lse: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """kvf_attend: the queries attend to every row the cache holds; nothing is appended."""
+               lse: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, softcap: float = 0.0,
+               slopes: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None,
+               end: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """kvf_attend: the queries attend to every row the cache holds; nothing is appended.  With any of softcap, slopes,
+        first, end kvf_attend_scored."""
         n = q.shape[0]
         assert q.is_cuda and q.is_contiguous() and q.dtype == self.torch_dtype
         if out is None:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        if scores is not None:
+            rc = load().kvf_attend_scored(self._h, q.data_ptr(), n, int(len(self) if pos0 is None else pos0), ctypes.byref(scores),
+                                          out.data_ptr(), lse.data_ptr() if lse is not None else None, _stream_ptr(stream))
+            if rc != KVF_OK:
+                raise KvfError(rc, "kvf_attend_scored")
+            return out
         rc = load().kvf_attend(self._h, q.data_ptr(), n, int(len(self) if pos0 is None else pos0), out.data_ptr(),
                                lse.data_ptr() if lse is not None else None, _stream_ptr(stream))
         if rc != KVF_OK:
             raise KvfError(rc, "kvf_attend")
         return out
+
+    def rotate(self, q: torch.Tensor, pos0: Optional[int] = None, out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """kvf_rotate_queries: the chunk's queries as a step at pos0 rotates them (default: the chunk just appended)."""
+        n = q.shape[0]
+        assert q.is_cuda and q.is_contiguous() and q.dtype == self.torch_dtype
+        if out is None:
+            out = torch.empty_like(q)
+        assert out.is_contiguous() and out.dtype == q.dtype and out.shape == q.shape
+        rc = load().kvf_rotate_queries(self._h, q.data_ptr(), n, int(len(self) - n if pos0 is None else pos0), out.data_ptr(), _stream_ptr(stream))
+        if rc != KVF_OK:
+            raise KvfError(rc, "kvf_rotate_queries")
+        return out
+
+    def mass(self, q_rot: torch.Tensor, lse: torch.Tensor, mass: Optional[torch.Tensor] = None, decay: float = 1.0,
+             out: Optional[torch.Tensor] = None, appended: bool = True, pos0: Optional[int] = None, softcap: float = 0.0,
+             slopes: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None, end: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """kvf_cache_mass: decay * mass plus the weight that the rotated queries [n, H, d] with denominators lse [n, H] give every
+        row; mass and out are [Hkv, >= len] fp32 (out may be mass; a new [Hkv, len] tensor by default)."""
+        n, rows, hkv = q_rot.shape[0], len(self), self.cfg.n_kv_heads
+        assert q_rot.is_cuda and q_rot.is_contiguous() and q_rot.dtype == self.torch_dtype
+        assert lse.is_cuda and lse.is_contiguous() and lse.dtype is torch.float32 and lse.numel() == n * self.cfg.n_q_heads
+        if out is None:
+            out = torch.empty((hkv, rows), dtype=torch.float32, device=q_rot.device)
+        for t in (mass, out):
+            assert t is None or (t.is_cuda and t.dtype is torch.float32 and t.dim() == 2 and t.shape[0] == hkv and t.shape[1] >= rows and t.stride(1) == 1)
+        if pos0 is None:
+            pos0 = max(rows - n, 0) if appended else rows
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        rc = load().kvf_cache_mass(self._h, q_rot.data_ptr(), n, int(appended), int(pos0), None if scores is None else ctypes.byref(scores),
+                                   lse.data_ptr(), None if mass is None else mass.data_ptr(), 0 if mass is None else mass.stride(0),
+                                   decay, out.data_ptr(), out.stride(0), _stream_ptr(stream))
+        if rc != KVF_OK:
+            raise KvfError(rc, "kvf_cache_mass")
+        return out
+
+    def evict(self, into: "Cache", mass: torch.Tensor, budget: int, n_sink: int = 0, n_recent: int = 0,
+              mass_out: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """kvf_cache_evict: `budget` rows of every KV head become the rows of `into`; returns their numbers [Hkv, budget]."""
+        hkv = self.cfg.n_kv_heads
+        if kept is None:
+            kept = torch.empty((hkv, budget), dtype=torch.int32, device=mass.device)
+        assert mass.is_cuda and mass.dtype is torch.float32 and mass.shape[0] == hkv and mass.shape[1] >= len(self) and mass.stride(1) == 1
+        assert kept.is_cuda and kept.dtype is torch.int32 and kept.is_contiguous() and kept.numel() == hkv * budget
+        assert mass_out is None or (mass_out.is_cuda and mass_out.dtype is torch.float32 and mass_out.shape[0] == hkv and
+                                    mass_out.shape[1] >= budget and mass_out.stride(1) == 1)
+        rc = load().kvf_cache_evict(self._h, into._h, mass.data_ptr(), mass.stride(0), n_sink, n_recent, budget,
+                                    None if mass_out is None else mass_out.data_ptr(), 0 if mass_out is None else mass_out.stride(0),
+                                    kept.data_ptr(), _stream_ptr(stream))
+        if rc != KVF_OK:
+            raise KvfError(rc, "kvf_cache_evict")
+        return kept
 
     def fold_step_host(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor,
                        pos0: Optional[int] = None, lse: Optional[torch.Tensor] = None,

@@ -10,6 +10,7 @@
 // KV head share each K/V tile) x 64 keys per iteration; 256 threads as a 16 x 16 grid, each thread
 // a 4 x 4 block of scores and a 4 x (d/16) block of the output.
 #include "kvfold_internal.h"
+#include "scores.cuh"
 
 namespace kvf {
 namespace {
@@ -37,7 +38,9 @@ template <> struct Ld<__nv_bfloat16> {
     }
 };
 
-template <typename T, int D>
+// kScored: scores capped, biased and masked by a range of rows per token (ScoreMods); a split is then an equal share of the key tiles
+// that the row tile's tokens see between them.
+template <typename T, int D, bool kScored>
 __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a) {
     constexpr int QS = D + 4;            // padded row stride of the Q and K tiles (floats)
     constexpr int SS = BN + 4;           // padded row stride of the probability tile
@@ -66,8 +69,26 @@ __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a
     const int nt_need = (int)((need + BN - 1) / BN) - wt.skip;
     const int nt_all = (int)((L + BN - 1) / BN) - wt.skip;
     const int per = (nt_all + a.splits - 1) / a.splits;
-    const int kt_begin = split * per;
-    const int kt_end = min(nt_need, kt_begin + per);
+    int kt_begin = split * per;
+    int kt_end = min(nt_need, kt_begin + per);
+    if constexpr (kScored) {
+        __shared__ int seen[2];          // first key tile that a token of mine sees, end of the last one
+        if (tid == 0) { seen[0] = INT_MAX; seen[1] = 0; }
+        __syncthreads();
+        const int tok = row0 / G + tid;
+        if (tok <= tok_last) {           // (at most 64 tokens)
+            const RowRange r = seen_rows(a.mods, tok, tok, P, L, a.self_rows);
+            if (r.begin < r.end) {
+                atomicMin(&seen[0], (int)(r.begin / BN));
+                atomicMax(&seen[1], (int)((r.end + BN - 1) / BN));
+            }
+        }
+        __syncthreads();
+        const int first = min(seen[0], seen[1]);
+        const int64_t span = seen[1] - first;
+        kt_begin = first + (int)(split * span / a.splits);
+        kt_end = first + (int)((split + 1) * span / a.splits);
+    }
 
     // Q tile -> shared (fp32)
     for (int idx = tid; idx < BM * (D / VEC); idx += kThreads) {
@@ -83,10 +104,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a
     }
 
     int64_t limit[4];   // keys with index < limit are visible to row 4*ty + i
+    int64_t begin[4];   // (kScored) from this one on
+    float slope[4];     // (kScored) in log2 units per row of distance
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         int tok = (row0 + 4 * ty + i) / G;
         limit[i] = tok < n ? P + (tok + 1) * a.self_rows : 0;
+        if constexpr (kScored) {
+            const RowRange r = tok < n ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, 0};
+            begin[i] = r.begin;
+            limit[i] = r.end;
+            slope[i] = a.mods.slopes && tok < n ? a.mods.slopes[kvh * G + (row0 + 4 * ty + i) % G] * kLog2e : 0.f;
+        }
     }
 
     float m[4], l[4], acc[4][NC * 4];
@@ -146,8 +175,14 @@ __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int64_t key = key0 + tx + 16 * j;
-                bool vis = key < limit[i] && (key >= a.win_lo || key < a.n_sink);
-                s[i][j] = vis ? s[i][j] * a.scale_log2 : -INFINITY;
+                bool vis = key < limit[i] && (kScored ? key >= begin[i] : key >= a.win_lo || key < a.n_sink);
+                float x = s[i][j] * a.scale_log2;
+                if constexpr (kScored) {
+                    if (a.mods.cap_out > 0.f) x = a.mods.cap_out * tanhf(s[i][j] * a.mods.cap_in);
+                    const int64_t at = a.mods.pos0 + (row0 + 4 * ty + i) / G - key;
+                    if (a.mods.slopes) x = fmaf(-slope[i], (float)(at < 0 ? -at : at), x);
+                }
+                s[i][j] = vis ? x : -INFINITY;
                 mx = fmaxf(mx, s[i][j]);
             }
 #pragma unroll
@@ -267,16 +302,21 @@ __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a) {
     if (c == 0 && a.lse) a.lse[row] = (M + log2f(den)) * 0.6931471805599453f;
 }
 
-template <typename T, int D>
-cudaError_t launch_simt_t(const AttnArgs &a, cudaStream_t s, int *grid_out) {
+template <typename T, int D, bool kScored>
+cudaError_t launch_simt_k(const AttnArgs &a, cudaStream_t s, int *grid_out) {
     constexpr size_t smem = sizeof(float) * (size_t)(BM * (D + 4) + BN * (D + 4) + BN * D);
     static_assert(BM * (BN + 4) <= BN * (D + 4), "probability tile must fit in the K tile");
-    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(attn_simt_kernel<T, D>), (int)smem);
+    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(attn_simt_kernel<T, D, kScored>), (int)smem);
     if (e != cudaSuccess) return e;
     dim3 grid((a.n * a.G + BM - 1) / BM, a.Hkv, a.splits);
     if (grid_out) *grid_out = grid.x * grid.y * grid.z;
-    attn_simt_kernel<T, D><<<grid, kThreads, smem, s>>>(a);
+    attn_simt_kernel<T, D, kScored><<<grid, kThreads, smem, s>>>(a);
     return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_simt_t(const AttnArgs &a, cudaStream_t s, int *grid_out) {
+    return a.scored ? launch_simt_k<T, D, true>(a, s, grid_out) : launch_simt_k<T, D, false>(a, s, grid_out);
 }
 
 }  // namespace

@@ -325,15 +325,18 @@ int64_t window_lo(const kvf_cache *c, int64_t prefix) {
 }
 
 // (`ragged`: the members' row counts are known on the device only, and with them which ranges a KV head has)
-Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t part_rows_cap = -1, bool one_launch = true, bool ragged = false) {
+// (`scored`: capped, biased or range-masked scores - not in one launch, and on the CUDA cores)
+Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t part_rows_cap = -1, bool one_launch = true, bool ragged = false,
+               bool scored = false) {
     if (part_rows_cap < 0) part_rows_cap = c->part_rows_cap;
     Plan p;
     p.qdec = p.small = false;
-    p.tc = c->tc || c->tc32;
+    p.tc = (c->tc || c->tc32) && !scored;
+    one_launch = one_launch && !scored;
     p.ngroups = p.ranks = 0;
     const int64_t L = prefix + n;
     const int Hkv = c->cfg.n_kv_heads;
-    if ((c->quant || c->tc) && c->window <= 0 && n * c->G <= attn_q8_decode_max_rows()) {
+    if ((c->quant || c->tc) && !scored && c->window <= 0 && n * c->G <= attn_q8_decode_max_rows()) {
         // one CTA per SM (all caches of a batch together), each inside one KV head (a multiple of the KV heads),
         // at least two key tiles each; a forced split count is the number of ranges per KV head
         const int64_t nt = (L + kKvTile - 1) / kKvTile;
@@ -649,14 +652,28 @@ bool disjoint_step(const kvf_cache *c, const void *q, const void *k_new, const v
     return true;
 }
 
+ScoreMods score_mods(const kvf_cache *c, const kvf_scores *sc, int64_t pos0) {
+    ScoreMods m = {};
+    m.pos0 = pos0;
+    if (!sc) return m;
+    if (sc->softcap > 0.0) {
+        m.cap_in = (float)(c->scale_log2 * 0.6931471805599453 / sc->softcap);
+        m.cap_out = (float)(sc->softcap * 1.4426950408889634);
+    }
+    m.slopes = sc->slopes;
+    m.first = sc->first;
+    m.end = sc->end;
+    return m;
+}
+
 kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void *v_new, int32_t n,
-                     int64_t pos0, void *out, float *lse, cudaStream_t st, int staging_set = -1) {
+                     int64_t pos0, void *out, float *lse, cudaStream_t st, int staging_set = -1, const kvf_scores *scores = nullptr) {
     const kvf_config &f = c->cfg;
     const int64_t P = c->len;
     // k_new == null: queries only (kvf_attend) - nothing is appended, every query row sees the P rows held
     const bool attend = k_new == nullptr;
     const int64_t L = attend ? P : P + n;                     // rows the step's queries can see at most
-    const Plan plan = make_plan(c, n, L - n, 1, -1, disjoint_step(c, q, k_new, v_new, n, out, lse));
+    const Plan plan = make_plan(c, n, L - n, 1, -1, disjoint_step(c, q, k_new, v_new, n, out, lse), false, scores != nullptr);
     const bool behind = c->comb_stream != nullptr;
     unsigned long long capture = 0;
     if (behind) {
@@ -682,11 +699,13 @@ kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void 
     ra.page_tables = nullptr;
     ra.prefixes = nullptr; ra.pos0s = nullptr; ra.ns = nullptr;
     ra.status = reinterpret_cast<int *>(c->workspace + c->lay.status);
-    ra.range_limit = c->tc32 ? 65504.f : 0.f;      // the fp32 tensor-core kernel computes on fp16 halves
+    ra.range_limit = c->tc32 && plan.tc ? 65504.f : 0.f;      // the fp32 tensor-core kernel computes on fp16 halves
     ra.sms = c->sm_count;
     ra.table = c->table;
 
     AttnArgs aa;
+    aa.scored = scores != nullptr;
+    aa.mods = score_mods(c, scores, pos0);
     aa.q_rot = ra.q_rot;
     aa.k_plane = ra.k_plane; aa.v_plane = ra.v_plane;
     aa.out = out; aa.lse = lse;
@@ -746,8 +765,8 @@ kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void 
         ProfScope ps(c, st, 1);
         if (plan.small) e = launch_fold_small(ra, aa, plan.cut, f.dtype, (f.flags & KVF_ROPE_INTERLEAVED) != 0, st);
         else if (plan.qdec) e = launch_attn_q8_decode(aa, c->maps, st);
-        else if (c->tc) e = launch_attn_tc(aa, c->maps, st);
-        else if (c->tc32) e = launch_attn_tc32(aa, st);
+        else if (plan.tc && c->tc) e = launch_attn_tc(aa, c->maps, st);
+        else if (plan.tc) e = launch_attn_tc32(aa, st);
         else e = launch_attn_simt(aa, f.dtype, st, nullptr);
     }
     if (e != cudaSuccess) return cuda_fail(e, "attention launch");
@@ -841,6 +860,48 @@ size_t page_bytes_of(const kvf_config *cfg) {
     if (cfg->flags & (KVF_CACHE_INT8 | KVF_CACHE_INT4))
         return rows * ((cfg->flags & KVF_CACHE_INT4) ? (size_t)cfg->head_dim / 2 : (size_t)cfg->head_dim) + rows * 4;
     return rows * (size_t)cfg->head_dim * elem_bytes(cfg->dtype);
+}
+
+kvf_status check_f32(const float *p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3u) ? KVF_ERR_INVALID_ARG : KVF_OK; }
+
+kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
+    if (!sc || !(sc->softcap >= 0.0) || std::isinf(sc->softcap)) return KVF_ERR_INVALID_ARG;
+    if ((sc->slopes && check_f32(sc->slopes)) || (sc->first && check_f32(reinterpret_cast<const float *>(sc->first))) ||
+        (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
+        return KVF_ERR_INVALID_ARG;
+    if (c->window > 0 || c->quant || c->page_table) return KVF_ERR_UNSUPPORTED;
+    return KVF_OK;
+}
+
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+bool overlap(const void *a, const void *b, size_t bytes) { return overlap(a, bytes, b, bytes); }
+
+// A row of `stride` floats for each KV head.
+size_t strided_bytes(const kvf_cache *c, int64_t stride) { return (size_t)c->cfg.n_kv_heads * (size_t)stride * 4; }
+
+// Bytes of a cache's storage, or of the pool it has pages of.
+size_t held_bytes(const kvf_cache *c) {
+    if (c->page_table) return (size_t)c->n_pool_pages * page_bytes_of(&c->cfg);
+    return 2 * c->plane_bytes + (c->quant ? 2 * (size_t)c->cfg.n_kv_heads * c->qp.scale_stride * 4 : 0);
+}
+
+RowPlanes row_planes(const kvf_cache *c) {
+    RowPlanes p = {};
+    p.k = c->storage;
+    p.v = c->storage + c->plane_bytes;
+    p.page_table = c->page_table;
+    p.capacity = c->cfg.capacity;
+    p.page_bytes = c->page_table ? (int64_t)page_bytes_of(&c->cfg) : 0;
+    p.row_bytes = c->quant ? c->cfg.head_dim * c->qp.bits / 8 : c->cfg.head_dim * (int)elem_bytes(c->cfg.dtype);
+    if (c->quant) {
+        p.k_scales = c->qp.k_scales;
+        p.v_scales = c->qp.v_scales;
+        p.scale_stride = c->qp.scale_stride;
+    }
+    return p;
 }
 
 kvf_status check_step(kvf_cache *c, int32_t n, int64_t pos0) {
@@ -983,6 +1044,130 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
     if (check_ptr(q) || check_ptr(out)) return KVF_ERR_INVALID_ARG;
     if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return KVF_ERR_INVALID_ARG;
     return step_impl(c, q, nullptr, nullptr, n_tokens, pos0, out, lse, static_cast<cudaStream_t>(cuda_stream));
+}
+
+kvf_status kvf_fold_step_scored(kvf_cache *c, const void *q, const void *k_new, const void *v_new, int32_t n_tokens, int64_t pos0,
+                                const kvf_scores *scores, void *out, float *lse, void *cuda_stream) {
+    kvf_status s = check_step(c, n_tokens, pos0);
+    if (s != KVF_OK) return s;
+    s = check_scores(c, scores);
+    if (s != KVF_OK) return s;
+    if (check_ptr(q) || check_ptr(k_new) || check_ptr(v_new) || check_ptr(out)) return KVF_ERR_INVALID_ARG;
+    if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return KVF_ERR_INVALID_ARG;
+    return step_impl(c, q, k_new, v_new, n_tokens, pos0, out, lse, static_cast<cudaStream_t>(cuda_stream), -1, scores);
+}
+
+kvf_status kvf_attend_scored(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos0, const kvf_scores *scores, void *out, float *lse,
+                             void *cuda_stream) {
+    if (!c) return KVF_ERR_INVALID_ARG;
+    if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0) return KVF_ERR_INVALID_ARG;
+    if (c->len < 1) return KVF_ERR_INVALID_ARG;
+    kvf_status s = check_scores(c, scores);
+    if (s != KVF_OK) return s;
+    if (check_ptr(q) || check_ptr(out)) return KVF_ERR_INVALID_ARG;
+    if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return KVF_ERR_INVALID_ARG;
+    return step_impl(c, q, nullptr, nullptr, n_tokens, pos0, out, lse, static_cast<cudaStream_t>(cuda_stream), -1, scores);
+}
+
+kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos0, void *q_rot, void *cuda_stream) {
+    if (!c) return KVF_ERR_INVALID_ARG;
+    if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0) return KVF_ERR_INVALID_ARG;
+    if (check_ptr(q) || check_ptr(q_rot)) return KVF_ERR_INVALID_ARG;
+    const kvf_config &f = c->cfg;
+    if (overlap(q, q_rot, (size_t)n_tokens * f.n_q_heads * f.head_dim * elem_bytes(f.dtype)) && q != q_rot) return KVF_ERR_INVALID_ARG;
+    RopeAppendArgs ra = {};
+    ra.q = q;
+    ra.q_rot = q_rot;
+    ra.capacity = f.capacity; ra.prefix = c->len; ra.pos0 = pos0;
+    ra.n = n_tokens; ra.H = f.n_q_heads; ra.Hkv = f.n_kv_heads; ra.d = f.head_dim;
+    ra.status = reinterpret_cast<int *>(c->workspace + c->lay.status);
+    ra.sms = c->sm_count;
+    ra.table = c->table;
+    const PdlScope pdl(dependent_launches());
+    const cudaError_t e = launch_rope_append(ra, f.dtype, (f.flags & KVF_ROPE_INTERLEAVED) != 0, 1, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(e, "rotate launch");
+    c->launches++;
+    return KVF_OK;
+}
+
+kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int32_t appended, int64_t pos0, const kvf_scores *scores,
+                          const float *lse, const float *mass_in, int64_t in_stride, float decay, float *mass_out, int64_t out_stride,
+                          void *cuda_stream) {
+    if (!c) return KVF_ERR_INVALID_ARG;
+    if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0 || c->len < 1 || (appended != 0 && appended != 1)) return KVF_ERR_INVALID_ARG;
+    if (appended && n_tokens > c->len) return KVF_ERR_INVALID_ARG;
+    if (!std::isfinite(decay)) return KVF_ERR_INVALID_ARG;
+    if (c->quant || c->page_table || c->window > 0) return KVF_ERR_UNSUPPORTED;
+    if (scores) {
+        const kvf_status s = check_scores(c, scores);
+        if (s != KVF_OK) return s;
+    }
+    if (check_ptr(q_rot) || check_f32(lse) || check_f32(mass_out) || (mass_in && check_f32(mass_in))) return KVF_ERR_INVALID_ARG;
+    if (out_stride < c->len || (mass_in && in_stride < c->len)) return KVF_ERR_INVALID_ARG;
+    const kvf_config &f = c->cfg;
+    // (an entry is read by the thread that writes it: in place, but not shifted)
+    if (mass_in && !(mass_in == mass_out && in_stride == out_stride) &&
+        overlap(mass_in, strided_bytes(c, in_stride), mass_out, strided_bytes(c, out_stride)))
+        return KVF_ERR_INVALID_ARG;
+    MassArgs a = {};
+    a.q_rot = q_rot;
+    a.k_plane = c->storage;
+    a.page_table = c->page_table;
+    a.page_elems = c->page_elems;
+    a.capacity = f.capacity;
+    a.lse = lse;
+    a.mass_in = mass_in; a.mass_out = mass_out;
+    a.in_stride = in_stride; a.out_stride = out_stride;
+    a.decay = decay;
+    a.rows = c->len;
+    a.held = appended ? c->len - n_tokens : c->len;
+    a.n = n_tokens; a.H = f.n_q_heads; a.Hkv = f.n_kv_heads; a.G = c->G; a.d = f.head_dim;
+    a.self_rows = appended;
+    a.status = reinterpret_cast<int *>(c->workspace + c->lay.status);
+    a.scale_log2 = c->scale_log2;
+    a.scored = scores != nullptr;
+    a.mods = score_mods(c, scores, pos0);
+    a.sms = c->sm_count;
+    const PdlScope pdl(dependent_launches());
+    const cudaError_t e = launch_mass_simt(a, f.dtype, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(e, "mass launch");
+    c->launches++;
+    return KVF_OK;
+}
+
+kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *mass, int64_t mass_stride, int64_t n_sink, int64_t n_recent,
+                           int64_t budget, float *mass_out, int64_t out_stride, int32_t *kept, void *cuda_stream) {
+    if (!from || !to || from == to) return KVF_ERR_INVALID_ARG;
+    const kvf_config &x = from->cfg, &y = to->cfg;
+    if (x.n_q_heads != y.n_q_heads || x.n_kv_heads != y.n_kv_heads || x.head_dim != y.head_dim || x.dtype != y.dtype ||
+        from->quant != to->quant || (from->quant && from->qp.bits != to->qp.bits) || from->device != to->device)
+        return KVF_ERR_INVALID_ARG;
+    if (n_sink < 0 || n_recent < 0 || budget < 1 || n_sink > budget || n_recent > budget - n_sink || budget > from->len) return KVF_ERR_INVALID_ARG;
+    if (budget > y.capacity) return KVF_ERR_CAPACITY;
+    if (check_f32(mass) || (mass_out && check_f32(mass_out)) || check_f32(reinterpret_cast<const float *>(kept))) return KVF_ERR_INVALID_ARG;
+    if (mass_stride < from->len || (mass_out && out_stride < budget)) return KVF_ERR_INVALID_ARG;
+    if (mass_out && overlap(mass, strided_bytes(from, mass_stride), mass_out, strided_bytes(from, out_stride))) return KVF_ERR_INVALID_ARG;
+    // two paged caches of one pool keep different pages of it (the caller's tables say so); nothing else may be shared
+    if (!(from->page_table && to->page_table && from->storage == to->storage && from->page_table != to->page_table) &&
+        overlap(from->storage, held_bytes(from), to->storage, held_bytes(to)))
+        return KVF_ERR_INVALID_ARG;
+    EvictArgs a = {};
+    a.from = row_planes(from);
+    a.to = row_planes(to);
+    a.mass = mass; a.mass_out = mass_out;
+    a.mass_stride = mass_stride; a.out_stride = out_stride;
+    a.kept = kept;
+    a.rows = from->len;
+    a.budget = budget; a.n_sink = n_sink; a.n_recent = n_recent;
+    a.zero_end = (budget + kKvTile - 1) / kKvTile * kKvTile;
+    if (a.zero_end > y.capacity && !to->page_table) a.zero_end = y.capacity;
+    a.Hkv = x.n_kv_heads;
+    const PdlScope pdl(dependent_launches());
+    const cudaError_t e = launch_evict(a, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(e, "evict launch");
+    to->launches += 2;
+    to->len = budget;
+    return KVF_OK;
 }
 
 kvf_status kvf_merge_partials(int32_t n_parts, int64_t n_rows, int32_t head_dim, kvf_dtype dtype, const void *parts_out,

@@ -135,6 +135,15 @@ struct RopeAppendArgs {
     RopeTable table;
 };
 
+// What a scored step does to its scores (kvf_scores): s = scale * (q . k) becomes softcap * tanh(s / softcap), then
+// s - slope[head] * |position of the token - row|; token i sees rows [first[i], end[i]).
+struct ScoreMods {
+    float cap_in, cap_out;           // scale / softcap and softcap * log2(e) (cap_out = 0: no cap)
+    const float *slopes;             // device [H] or null
+    const int32_t *first, *end;      // device [n] or null (row 0; every row up to the token's own)
+    int64_t pos0;                    // position of token 0
+};
+
 // Arguments shared by the attention kernels and the combine kernel.
 struct AttnArgs {
     const void *q_rot;               // [n][H][d]
@@ -183,6 +192,8 @@ struct AttnArgs {
     int32_t self_rows;               // 1: a fold step - the chunk's own rows are in the cache, token i sees rows < prefix + i + 1;
                                      // 0: queries only (kvf_attend) - nothing was appended, every token sees rows < prefix
     float scale_log2;                // softmax scale * log2(e)
+    int32_t scored;                  // 1: mods below apply (kvf_fold_step_scored, kvf_attend_scored)
+    ScoreMods mods;
     // tensor-core paths, when the host knows the row count (no ragged batch): first and last group whose
     // range of the (KV head, key tile) line touches KV head h, for h < kRangeHeads (see group_range)
     int32_t range_valid;
@@ -279,6 +290,61 @@ cudaError_t launch_attn_q8_decode(const AttnArgs &a, const TcMaps &maps, cudaStr
 // Merge of attention results over disjoint sets of cache rows (merge_parts.cu).
 cudaError_t launch_merge_parts(int n_parts, int64_t n_rows, int d, bool f32, const void *parts_out, const float *parts_lse,
                                void *out, float *lse, cudaStream_t s);
+
+// Attention weight of a chunk's queries on the rows of a cache (attn_mass.cu).
+struct MassArgs {
+    const void *q_rot;               // [n][H][d]
+    const void *k_plane;             // [Hkv][capacity][d], or the pool (page_table)
+    const int32_t *page_table;
+    int64_t page_elems, capacity;
+    const float *lse;                // [n][H], natural log
+    const float *mass_in;            // [Hkv][in_stride] or null (zeros)
+    float *mass_out;                 // [Hkv][out_stride]
+    int64_t in_stride, out_stride;
+    float decay;
+    int64_t rows;                    // rows the cache holds
+    int64_t held;                    // rows whose weight is carried over (those from here on start from zero)
+    int32_t n, H, Hkv, G, d;
+    int32_t self_rows;               // 1: the queries are those of the last n rows; 0: they see every row
+    int *status;
+    float scale_log2;
+    int32_t scored;
+    ScoreMods mods;
+    int32_t sms;
+};
+cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s);
+
+// Eviction (evict.cu).  Where the rows of a cache's planes live, in bytes: contiguous planes [Hkv][capacity][row bytes] or pages of
+// 128 rows of every KV head; quantised storage has a fp32 scale per row besides.
+struct RowPlanes {
+    char *k, *v;                     // planes, or the K and the V block of page 0
+    float *k_scales, *v_scales;      // or null
+    const int32_t *page_table;       // null = contiguous
+    int64_t capacity, page_bytes, scale_stride;
+    int32_t row_bytes;
+#ifdef __CUDACC__
+    __device__ __forceinline__ int64_t offset(int g, int64_t row) const {
+        if (page_table == nullptr) return ((int64_t)g * capacity + row) * row_bytes;
+        return page_table[row / kKvTile] * page_bytes + ((int64_t)g * kKvTile + row % kKvTile) * row_bytes;
+    }
+    __device__ __forceinline__ int64_t scale_offset(int g, int64_t row) const {
+        if (page_table == nullptr) return (int64_t)g * scale_stride + row;
+        return page_table[row / kKvTile] * (page_bytes / 4) + (int64_t)g * kKvTile + row % kKvTile;
+    }
+#endif
+};
+struct EvictArgs {
+    RowPlanes from, to;
+    const float *mass;               // [Hkv][mass_stride]
+    float *mass_out;                 // [Hkv][out_stride] or null
+    int64_t mass_stride, out_stride;
+    int32_t *kept;                   // [Hkv][budget]: rows of `from`, ascending
+    int64_t rows;                    // rows `from` holds
+    int64_t budget, n_sink, n_recent;
+    int64_t zero_end;                // value rows [budget, zero_end) of `to` are cleared
+    int32_t Hkv;
+};
+cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s);
 
 bool attn_tc32_supported(int dtype, int d, int G);
 int attn_tc32_row_blocks(int n, int G);   // 128-row blocks per KV head = grid.x

@@ -1,0 +1,214 @@
+"""The attention weight of a chunk and the eviction by it, against their plain statements."""
+import math
+
+import pytest
+import torch
+
+from paper_2605_12471_b200 import binding
+from tests import scored
+from tests.test_scored_gpu import BASE, HEADS, chunk, documents, make, slopes_of
+
+pytestmark = pytest.mark.gpu
+
+
+def lse_of(q, keys, seen, scale, pos0, **kw):
+    s, _ = scored.scores(q, keys, scale, pos0, kw.get("softcap", 0.0), kw.get("slopes"))
+    row = torch.arange(keys.shape[1], device=q.device)
+    hidden = ~((row >= seen[0][:, None]) & (row < seen[1][:, None]))
+    return torch.logsumexp(s.masked_fill(hidden[:, None], -math.inf), -1).float().contiguous()
+
+
+@pytest.mark.parametrize("n,prefix", [(1, 0), (1, 1), (1, 1000), (3, 129), (6, 5000), (33, 515), (64, 0), (129, 127), (300, 1111), (1000, 40)])
+@pytest.mark.parametrize("heads,dtype", HEADS)
+def test_mass_matches_its_statement(heads, dtype, n, prefix):
+    rows = prefix + n
+    for seed, name in enumerate(["plain", "cap", "all", "attend"]):
+        cache, gen = make(heads, dtype, rows + 9, n, prefix=rows, seed=seed)
+        q = chunk(cache, gen, n, scale=2.0)[0]
+        kw = {}
+        if name in ("cap", "all"):
+            kw["softcap"] = 5.0
+        if name == "all":
+            kw["slopes"] = slopes_of(heads[0])
+            kw["first"], kw["end"] = documents(n, prefix, gen)
+        appended = name != "attend"
+        seen = scored.ranges(n, rows, prefix if appended else rows, appended, kw.get("first"), kw.get("end"))
+        scale, pos0 = 1 / math.sqrt(heads[2]), prefix if appended else rows
+        keys = cache.k_plane()[:, :rows]
+        lse = lse_of(q.double(), keys, seen, scale, pos0, **kw)
+        before = torch.rand((heads[1], rows + 9), generator=gen, device="cuda")
+        if appended:
+            before[:, prefix:] = math.nan                # (the step's own rows start from zero)
+        decay = [1.0, 0.5, 0.0, 1.0][seed]
+        out = torch.full((heads[1], rows + 4), -7.0, device="cuda")
+        cache.mass(q, lse, mass=before, decay=decay, out=out, appended=appended, **kw)
+        want, bound = scored.mass(q, keys, lse, seen, scale, pos0, kw.get("softcap", 0.0), kw.get("slopes"), before, decay,
+                                  prefix if appended else rows, dtype == "bf16" and heads[2] == 128)
+        off = (out[:, :rows].double() - want).abs()
+        assert bool((off <= bound).all()), (name, float((off / bound).max()))
+        assert bool((out[:, rows:] == -7.0).all())       # nothing behind the last row
+        assert cache.status() == binding.KVF_OK
+
+
+def test_mass_in_place_and_without_a_start():
+    cache, gen = make((32, 8, 128), "bf16", 2000, 256, prefix=1500, seed=1)
+    q = chunk(cache, gen, 100)[0]
+    lse = torch.randn((100, 32), generator=gen, device="cuda") + 8
+    fresh = cache.mass(q, lse)
+    assert fresh.shape == (8, 1500)
+    held = torch.rand((8, 2000), generator=gen, device="cuda")
+    want = torch.where(torch.arange(2000, device="cuda") < 1400, held * 0.25, 0.0)[:, :1500] + fresh
+    cache.mass(q, lse, mass=held, decay=0.25, out=held)
+    assert float(((held[:, :1500] - want).abs() / (want + 1e-6)).max()) <= 2.0 ** -22
+    # bit for bit the same again
+    assert torch.equal(cache.mass(q, lse), fresh)
+
+
+def test_mass_of_a_step_adds_up_to_its_tokens():
+    """fold, rotate, mass: the weights of a step sum to one for every token and query head."""
+    for heads, dtype in HEADS:
+        n, prefix = 60, 700
+        cache, gen = make(heads, dtype, 800, n, prefix=prefix, seed=2)
+        q, k, v = chunk(cache, gen, n)
+        lse = torch.empty((n, heads[0]), device="cuda")
+        cache.fold_step(q, k, v, lse=lse, softcap=10.0)
+        mass = cache.mass(cache.rotate(q), lse, softcap=10.0)
+        want = n * heads[0] / heads[1]
+        # (scores of fold and mass come from the same rounded queries; the denominators are fp32)
+        assert float((mass.double().sum(1) - want).abs().max()) <= 1e-4 * want
+
+
+def test_rotated_queries_are_the_rotation():
+    for heads, dtype in HEADS:
+        cache, gen = make(heads, dtype, 4000, 50, prefix=3000, seed=3)
+        q = chunk(cache, gen, 50)[0]
+        want = scored.turned(q, 2950, BASE)
+        u = scored.U[cache.torch_dtype]
+        size = scored.turned(q.abs(), 0, BASE).abs().amax() * 4
+        got = cache.rotate(q)
+        assert float((got.double() - want).abs().max()) <= u * float(want.abs().max()) + 2.0 ** -22 * float(size)
+        inplace = q.clone()
+        assert torch.equal(cache.rotate(inplace, out=inplace), got)
+
+
+SHAPES = [(1, 1, 0, 0), (5, 3, 0, 0), (130, 130, 4, 20), (130, 24, 4, 20), (1000, 1, 0, 0), (1000, 999, 3, 0), (4097, 2000, 4, 700), (33000, 8193, 1, 256),
+          (70001, 35000, 0, 1), (460001, 1234, 4, 1000)]
+
+
+def rows_of(cache, kv):
+    if isinstance(cache, binding.PagedCache):
+        table = cache.page_table.long()
+        if cache.cfg.flags & (binding.KVF_CACHE_INT8 | binding.KVF_CACHE_INT4):
+            codes = cache.page_codes(kv)[table].permute(1, 0, 2, 3).reshape(cache.cfg.n_kv_heads, -1, cache.cfg.head_dim)
+            scale = cache.page_scales(kv)[table].permute(1, 0, 2).reshape(cache.cfg.n_kv_heads, -1)
+            return codes, scale
+        return cache.page_rows(kv)[table].permute(1, 0, 2, 3).reshape(cache.cfg.n_kv_heads, -1, cache.cfg.head_dim), None
+    plane = cache.v_plane() if kv else cache.k_plane()
+    return plane, cache.scales(kv) if cache.cfg.flags & (binding.KVF_CACHE_INT8 | binding.KVF_CACHE_INT4) else None
+
+
+def same_rows(src, dst, kept):
+    head = torch.arange(kept.shape[0], device="cuda")[:, None]
+    for kv in (0, 1):
+        (a, sa), (b, sb) = rows_of(src, kv), rows_of(dst, kv)
+        assert torch.equal(a[head, kept.long()], b[:, :kept.shape[1]])
+        if sa is not None:
+            assert torch.equal(sa[head, kept.long()], sb[:, :kept.shape[1]])
+
+
+@pytest.mark.parametrize("rows,budget,sinks,recent", SHAPES)
+@pytest.mark.parametrize("heads,dtype", [((4, 2, 128), "bf16"), ((3, 3, 64), "f32")])
+def test_eviction_keeps_what_counts_most(heads, dtype, rows, budget, sinks, recent):
+    src, gen = make(heads, dtype, rows, 1, prefix=rows, seed=rows)
+    dst, _ = make(heads, dtype, budget + 3, 1)
+    dst.storage.fill_(0xFF)                                        # NaN everywhere
+    mass = (torch.randn((heads[1], rows + 1), generator=gen, device="cuda") * 3).exp().mul_(8).round_().div_(8)     # many alike
+    out = torch.full((heads[1], budget + 2), -1.0, device="cuda")
+    kept = src.evict(dst, mass, budget, n_sink=sinks, n_recent=recent, mass_out=out)
+    assert len(dst) == budget and len(src) == rows
+    assert torch.equal(kept.cpu(), scored.kept_rows(mass, rows, sinks, recent, budget))
+    same_rows(src, dst, kept)
+    head = torch.arange(heads[1], device="cuda")[:, None]
+    assert torch.equal(out[:, :budget], mass[head, kept.long()]) and bool((out[:, budget:] == -1).all())
+    # value rows behind the last one are zeros up to the tile's end, as after an append
+    end = min((budget + 127) // 128 * 128, budget + 3)
+    assert bool((dst.v_plane()[:, budget:end] == 0).all())
+
+
+def test_eviction_of_odd_weights():
+    """Ties, signs, infinities and NaN: a total order, the lower row first."""
+    rows, budget = 700, 300
+    for k, fill in enumerate([lambda m: m.zero_(), lambda m: m.fill_(math.nan), lambda m: m.neg_(),
+                              lambda m: m.masked_fill_(torch.rand_like(m) < 0.6, math.nan),
+                              lambda m: m.masked_fill_(torch.rand_like(m) < 0.2, math.inf).masked_fill_(torch.rand_like(m) < 0.7, -math.inf),
+                              lambda m: m.mul_(0).copysign_(torch.randn_like(m)), lambda m: m.mul_(1e-42)]):
+        src, gen = make((4, 2, 128), "bf16", rows, 1, prefix=rows, seed=k)
+        dst, _ = make((4, 2, 128), "bf16", rows, 1)
+        mass = torch.randn((2, rows), generator=gen, device="cuda")
+        fill(mass)
+        kept = src.evict(dst, mass, budget, n_sink=2, n_recent=10)
+        assert torch.equal(kept.cpu(), scored.kept_rows(mass, rows, 2, 10, budget)), k
+        same_rows(src, dst, kept)
+
+
+@pytest.mark.parametrize("flag", [0, binding.KVF_CACHE_INT8, binding.KVF_CACHE_INT4])
+@pytest.mark.parametrize("paged", [(False, False), (True, True), (False, True), (True, False)])
+def test_eviction_of_every_storage(flag, paged):
+    rows, budget, h, kv = 517, 260, 8, 2
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    cfg = binding.make_config(h, kv, 128, "bf16", 640, 640, rope_base=BASE, flags=flag)
+    pool = torch.zeros(binding.paged_pool_bytes(cfg, 12), dtype=torch.uint8, device="cuda")
+    tables = torch.randperm(12, generator=gen, device="cuda").to(torch.int32)
+
+    def one(is_paged, which):
+        return binding.PagedCache(cfg, pool, 12, tables[5 * which:5 * which + 5]) if is_paged else binding.Cache(cfg)
+
+    src, dst = one(paged[0], 0), one(paged[1], 1)
+    q, k, v = (torch.randn((rows, heads, 128), generator=gen, device="cuda").bfloat16() for heads in (h, kv, kv))
+    src.fold_step(q, k, v)
+    held = lambda: [x[:, :rows].clone() for x in rows_of(src, 0) + rows_of(src, 1) if x is not None]      # (rows behind hold anything)
+    before = held()
+    mass = torch.rand((kv, rows), generator=gen, device="cuda")
+    kept = src.evict(dst, mass, budget, n_sink=3, n_recent=50)
+    assert torch.equal(kept.cpu(), scored.kept_rows(mass, rows, 3, 50, budget))
+    same_rows(src, dst, kept)
+    assert all(torch.equal(a, b) for a, b in zip(before, held()))
+    # the next step on the smaller cache attends to the kept rows (and is told its position)
+    q, k, v = (torch.randn((3, heads, 128), generator=gen, device="cuda").bfloat16() for heads in (h, kv, kv))
+    out = dst.fold_step(q, k, v, pos0=rows)
+    assert len(dst) == budget + 3 and bool(torch.isfinite(out.float()).all()) and dst.status() == binding.KVF_OK
+    if not flag and not paged[1]:
+        seen = scored.ranges(3, budget + 3, budget, True)
+        want, _, bound, _ = scored.attend(scored.turned(q, rows, BASE), dst.k_plane()[:, :budget + 3], dst.v_plane()[:, :budget + 3], seen, 1 / math.sqrt(128), rows)
+        assert bool(((out.double() - want).abs() <= bound).all())
+
+
+def test_a_bounded_fold():
+    """The loop the operators are for: fold a chunk, add up its weights, cut back to the budget, go on."""
+    h, kv, budget, n = 8, 2, 300, 64
+    caches = [make((h, kv, 128), "bf16", budget + n, n)[0] for _ in range(2)]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    mass = torch.zeros((kv, budget + n), device="cuda")
+    spare = torch.zeros_like(mass)
+    pos = 0
+    for step in range(9):
+        here, there = caches
+        q, k, v = chunk(here, gen, n)
+        lse = torch.empty((n, h), device="cuda")
+        out = here.fold_step(q, k, v, pos0=pos, lse=lse, softcap=30.0)
+        prefix = len(here) - n
+        seen = scored.ranges(n, len(here), prefix, True)
+        keys, values = here.k_plane()[:, :len(here)], here.v_plane()[:, :len(here)]
+        want, _, bound, _ = scored.attend(scored.turned(q, pos, BASE), keys, values, seen, 1 / math.sqrt(128), pos, 30.0)
+        assert bool(((out.double() - want).abs() <= bound).all())
+        q_rot = here.rotate(q, pos0=pos)
+        before = mass.clone()
+        here.mass(q_rot, lse, mass=mass, decay=0.9, out=mass, softcap=30.0)
+        sums, off = scored.mass(q_rot, keys, lse, seen, 1 / math.sqrt(128), pos, 30.0, mass_in=before, decay=0.9, held=prefix)
+        assert bool(((mass[:, :len(here)].double() - sums).abs() <= off).all())
+        pos += n
+        if len(here) > budget:
+            kept = here.evict(there, mass, budget, n_sink=4, n_recent=n, mass_out=spare)
+            assert torch.equal(kept.cpu(), scored.kept_rows(mass, len(here), 4, n, budget))
+            caches, mass, spare = caches[::-1], spare, mass
+    assert all(c.status() == binding.KVF_OK for c in caches)
