@@ -61,6 +61,7 @@
 #include "kvfold_internal.h"
 #include "sm100_ptx.cuh"
 #include "quant_expand.cuh"
+#include "scores.cuh"
 
 namespace kvf {
 namespace {
@@ -278,7 +279,9 @@ __device__ __forceinline__ void value_fragment(const uint32_t (&w)[4][BITS / 2],
     }
 }
 
-template <int BITS, int NB>
+// kScored (bf16 rows): capped or biased scores, a range of rows per token (ScoreMods); the ranges' key tiles, those that a token of the
+// step sees, are cut among a KV head's CTAs as all of them are without.
+template <int BITS, int NB, bool kScored = false>
 __global__ void __launch_bounds__(Geo<BITS, NB>::kThreads, 1)
 attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using Gm = Geo<BITS, NB>;
@@ -311,8 +314,32 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
     const int64_t line = (int64_t)a.Hkv * nt_all;
     const int64_t lin0 = group * line / a.ngroups, lin1 = (group + 1) * line / a.ngroups;
     const int kvh = (int)(lin0 / nt_all);
-    const int kt0 = (int)(lin0 - (int64_t)kvh * nt_all);
-    const int ntiles = (int)(lin1 - lin0);         // a multiple of the KV heads cuts the line inside heads
+    int kt0 = (int)(lin0 - (int64_t)kvh * nt_all);
+    int ntiles = (int)(lin1 - lin0);         // a multiple of the KV heads cuts the line inside heads
+    int64_t all_from = 0, all_to = L;        // (kScored) rows that every token sees
+    if constexpr (kScored) {
+        // (a token sees what an earlier kernel may have written down: nothing can be set up ahead of that)
+        if (a.mods.first || a.mods.end) {
+            pdl_wait();
+            int64_t some_from = L, some_to = 0;
+            for (int tok = 0; tok < n; ++tok) {               // (16 at most)
+                const RowRange r = seen_rows(a.mods, (int64_t)cb * nmax + tok, tok, P, L, a.self_rows);
+                if (r.begin < r.end) {
+                    some_from = min(some_from, r.begin);
+                    some_to = max(some_to, r.end);
+                }
+                all_from = max(all_from, r.begin);
+                all_to = min(all_to, r.end);
+            }
+            const int t0 = (int)(some_from / kKeysPerTile), t1 = (int)((some_to + kKeysPerTile - 1) / kKeysPerTile);
+            const int64_t span = t1 > t0 ? t1 - t0 : 0;
+            const int at = kt0;
+            kt0 = t0 + (int)(at * span / nt_all);
+            ntiles = t0 + (int)((at + ntiles) * span / nt_all) - kt0;
+        } else {
+            all_to = P + a.self_rows;
+        }
+    }
     if (ntiles <= 0) {
         // A shorter member of a ragged batch (or a forced split count) can leave a range without a tile: an
         // empty partial, for the merge reads every slot between a head's first and last range.
@@ -323,6 +350,15 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
                 const int64_t prow = (int64_t)cb * a.part_rows + (int64_t)(group + kvh) * slot_rows + (r / G) * a.Gp + r % G;
                 reinterpret_cast<float4 *>(a.part_o + prow * kD)[c4] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (c4 == 0) a.part_lse[prow] = -INFINITY;
+            }
+        if (kScored && direct)                     // (no token sees anything)
+            for (int item = threadIdx.x; item < nG * (kD / 8); item += blockDim.x) {
+                const int r = item / (kD / 8), c8 = item % (kD / 8);
+                const int64_t row = ((int64_t)cb * nmax + r / G) * a.H + kvh * G + r % G;
+                uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.out) + row * (kD * (a.out_f32 ? 4 : 2))) + c8 * (a.out_f32 ? 2 : 1);
+                dst[0] = make_uint4(0u, 0u, 0u, 0u);
+                if (a.out_f32) dst[1] = make_uint4(0u, 0u, 0u, 0u);
+                if (c8 == 0 && a.lse) a.lse[row] = -INFINITY;
             }
         return;
     }
@@ -491,6 +527,25 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) limit[nb][e] = BITS == 16 ? limit_of(nb, e) : 0;
+        // (kScored) rows [begin, limit) of the cache, the head's slope in log2 units, and the token's position
+        int begin[NB][2];
+        float slope[NB][2];
+        if constexpr (kScored) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int R = 8 * nb + 2 * t4 + e, tok = R / G;
+                    RowRange r = {0, (int64_t)INT_MAX};
+                    slope[nb][e] = 0.f;
+                    if (R < nG) {
+                        r = seen_rows(a.mods, (int64_t)cb * nmax + tok, tok, P, L, a.self_rows);
+                        if (a.mods.slopes) slope[nb][e] = a.mods.slopes[kvh * G + R % G] * kLog2e;
+                    }
+                    begin[nb][e] = (int)r.begin;
+                    limit[nb][e] = (int)min(r.end, (int64_t)INT_MAX);
+                }
+        }
         // softmax scale * log2(e) of query rows 8 nb + 2 t + {0, 1} (whose scaling the threads of those g know)
         float sl2[NB][2];
 #pragma unroll
@@ -558,8 +613,38 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sacc[j][nb][e] *= BITS == 16 ? sl2[nb][e & 1] : row_scale[j][e >> 1] * sl2[nb][e & 1];
-            if (key_h + 64 > P) {
+                    for (int e = 0; e < 4; ++e) {
+                        if (kScored && a.mods.cap_out > 0.f) sacc[j][nb][e] = cap_any(a.mods, sacc[j][nb][e]);
+                        else sacc[j][nb][e] *= BITS == 16 ? sl2[nb][e & 1] : row_scale[j][e >> 1] * sl2[nb][e & 1];
+                    }
+            if constexpr (kScored) {
+                if (a.mods.slopes) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            // distance of my first key (key g of the 64)
+                            const float at = (float)(a.mods.pos0 + (8 * nb + 2 * t4 + e) / G - key_h - g);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                sacc[j][nb][e] = fmaf(-slope[nb][e], fabsf(at - 16.f * j), sacc[j][nb][e]);
+                                sacc[j][nb][2 + e] = fmaf(-slope[nb][e], fabsf(at - 16.f * j - 8.f), sacc[j][nb][2 + e]);
+                            }
+                        }
+                }
+                if (key_h < all_from || key_h + 64 > all_to) {
+                    const int key = (int)key_h + g;
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (key + 16 * j < begin[nb][e] || key + 16 * j >= limit[nb][e]) sacc[j][nb][e] = -INFINITY;
+                                if (key + 16 * j + 8 < begin[nb][e] || key + 16 * j + 8 >= limit[nb][e]) sacc[j][nb][2 + e] = -INFINITY;
+                            }
+                }
+            } else if (key_h + 64 > P) {
                 const int rel = (int)(key_h - P) + g;               // my first key, counted from P (> -64)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
@@ -793,6 +878,7 @@ cudaError_t launch_attn_q8_decode(const AttnArgs &a, const TcMaps &maps, cudaStr
     const int bits = a.quant_bits ? a.quant_bits : 16;              // 16: plain bf16 rows
     auto kernel = bits == 4 ? (wide ? attn_q8_decode_kernel<4, 2> : attn_q8_decode_kernel<4, 1>)
                 : bits == 8 ? (wide ? attn_q8_decode_kernel<8, 2> : attn_q8_decode_kernel<8, 1>)
+                : a.scored  ? (wide ? attn_q8_decode_kernel<16, 2, true> : attn_q8_decode_kernel<16, 1, true>)
                             : (wide ? attn_q8_decode_kernel<16, 2> : attn_q8_decode_kernel<16, 1>);
     const uint32_t smem = bits == 4 ? (wide ? Geo<4, 2>::kSmem : Geo<4, 1>::kSmem)
                         : bits == 8 ? (wide ? Geo<8, 2>::kSmem : Geo<8, 1>::kSmem) : (wide ? Geo<16, 2>::kSmem : Geo<16, 1>::kSmem);

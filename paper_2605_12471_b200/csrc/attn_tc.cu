@@ -91,6 +91,7 @@
 #include "kvfold_internal.h"
 #include "sm100_ptx.cuh"
 #include "quant_expand.cuh"
+#include "scores.cuh"
 
 namespace kvf {
 namespace {
@@ -146,6 +147,7 @@ struct Ctl {
     int abort;
     long long clk0;                // start of the CTA in SM cycles and in nanoseconds (the timed CTA only)
     unsigned long long ns0;
+    int seen[2];                   // (kScored) first key tile that a token of the row pair sees, end of the last one
 };
 static_assert(B_COUNT <= 40, "control block holds 40 barriers");
 
@@ -211,6 +213,21 @@ __device__ __forceinline__ void exp_half(const uint32_t *v, uint32_t *p, float2 
     }
 }
 
+// The same where the scores are still to be capped, by the small polynomial, whose last product takes the reference along.
+__device__ __forceinline__ void exp_half_small(const ScoreMods &m, const uint32_t *v, uint32_t *p, float2 negv, float2 &acc0, float2 &acc1) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+        const float2 s = make_float2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+        const float2 x = __ffma2_rn(s, cap_small_over(m, s), negv);
+        float2 e;
+        e.x = ex2(x.x);
+        e.y = ex2(x.y);
+        if (c & 1) acc1 = __fadd2_rn(acc1, e);
+        else acc0 = __fadd2_rn(acc0, e);
+        p[c] = pack_bf16(e.x, e.y);
+    }
+}
+
 // kWindow = false compiles the sink + window arithmetic out (launched whenever win_lo == 0).
 // kQuant (0, 8 or 4 bits): map_k / map_v describe int8 or int4 code planes; the producer brings raw code tiles into their own
 // ring and warps 12-15 (one thread per key row) expand each to the swizzled bf16 tile the MMAs read,
@@ -222,9 +239,12 @@ __device__ __forceinline__ void exp_half(const uint32_t *v, uint32_t *p, float2 
 // when every row pair has two row tiles (a chunk of a multiple of 512 / G tokens).
 // kEarly (bf16 rows, chunks of two row tiles): Q K^T of the next key tile is issued under the softmax of the
 // current one, see the issuer.
+// kScored (bf16 rows, no window): capped or biased scores, a range of rows per token (ScoreMods).  Scores are brought to log2 units
+// before the softmax.  With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the
+// line of all tiles is.
 // kRanks (bf16 rows, two streams): a cluster of that many CTAs has one row tile of one KV head, each an equal share of its key
 // tiles, and writes the output: no partial results, no merge kernel.  See the end of the kernel.
-template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0>
+template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0, bool kScored = false>
 __global__ void __launch_bounds__(kQuant ? kThreadsQ8 : kThreads, 1)
 attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v) {
@@ -289,6 +309,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
     const int64_t lin0 = group * line / a.ngroups, lin1 = (group + 1) * line / a.ngroups;
     const int kvh_first = kRanks ? group / kRanks : (int)(lin0 / ntv);
     // piece k of this CTA: KV head kvh_first + k, tiles [kt0, kt0 + ntiles)
+    int span0 = 0, span = -1;     // (kScored, ranges given) the row pair's key tiles [span0, span0 + span)
     auto piece = [&](int kvh, int &kt0, int &ntiles) -> bool {
         if (kRanks) {
             kt0 = (int)rank * nt_need / (kRanks ? kRanks : 1);
@@ -298,6 +319,12 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
         const int64_t b = (int64_t)kvh * ntv;
         if (kvh >= a.Hkv || b >= lin1) return false;
         kt0 = max((int)(max(lin0, b) - b) - pcost, 0);
+        if (kScored && span >= 0) {
+            const int kt1 = max((int)(min(lin1, b + ntv) - b) - pcost, 0);
+            kt0 = span0 + (int)((int64_t)kt0 * span / nt_all);
+            ntiles = span0 + (int)((int64_t)kt1 * span / nt_all) - kt0;
+            return true;
+        }
         const int kt1 = min(max((int)(min(lin1, b + ntv) - b) - pcost, 0), nt_need);
         ntiles = kt1 - kt0;
         return true;
@@ -323,6 +350,10 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
         mbar_init(bar(B_DRAIN0), 1);
         mbar_init(bar(B_DRAIN0 + 1), 1);
         ctl->abort = 0;
+        if (kScored) {
+            ctl->seen[0] = INT_MAX;
+            ctl->seen[1] = 0;
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -337,6 +368,21 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
     tc_fence_after();
     pdl_wait();   // nothing above reads what an earlier kernel wrote; from here on the rotated chunk is read
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&ctl->tmem_base);
+    if constexpr (kScored) {
+        if (a.mods.first || a.mods.end) {          // (uniform: the whole CTA comes here, or none of it)
+            const int tok = row0 / G + (int)threadIdx.x;            // (a row pair has 256 tokens at most)
+            if (tok <= tok_last) {
+                const RowRange r = seen_rows(a.mods, (int64_t)cb * nmax + tok, tok, P, L, a.self_rows);
+                if (r.begin < r.end) {
+                    atomicMin(&ctl->seen[0], (int)(r.begin / kRows));
+                    atomicMax(&ctl->seen[1], (int)((r.end + kRows - 1) / kRows));
+                }
+            }
+            __syncthreads();
+            span0 = min(ctl->seen[0], ctl->seen[1]);
+            span = ctl->seen[1] - span0;
+        }
+    }
     // One CTA times itself in SM cycles and in nanoseconds: the ratio is the clock the launch ran at
     // (the last row pair: it sees the most keys of the chunk itself, so no CTA of the launch runs longer)
     const bool clocked = qpair == pairs - 1 && group == 0 && blockIdx.z == 0 && threadIdx.x == 0;
@@ -705,8 +751,20 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
         // a key tile whose rows all lie below this needs no mask in any row of the warp (rows ascend, so the first
         // row of the warp sees least)
         const int tok_w = (row0 + (streams == 2 ? 0 : i * kRows) + (warp & 3) * 32) / G;
-        const int64_t clear = tok_w < n ? P + (tok_w + 1) * a.self_rows : ((int64_t)1 << 62);
-        const float sl2 = a.scale_log2;
+        int64_t limit_s = limit, begin_s = 0;
+        int64_t clear = tok_w < n ? P + (tok_w + 1) * a.self_rows : ((int64_t)1 << 62);
+        int64_t clear_from = 0;        // (kScored) ... and all from this one on
+        if constexpr (kScored) {
+            if (valid) {
+                const RowRange seen = seen_rows(a.mods, (int64_t)cb * nmax + tok, tok, P, L, a.self_rows);
+                limit_s = seen.end;
+                begin_s = seen.begin;
+            }
+            // (row numbers are below 2^31; a row past the chunk's end has no limits)
+            clear = (int64_t)__reduce_min_sync(0xffffffffu, (int)min(limit_s, (int64_t)INT_MAX));
+            clear_from = (int64_t)__reduce_max_sync(0xffffffffu, (int)begin_s);
+        }
+        const float sl2 = kScored ? 1.f : a.scale_log2;          // (kScored: scores come in log2 units)
         const float2 sl2v = make_float2(sl2, sl2);
         const int64_t nG = (int64_t)nmax * G;                 // rows of a partial slot
 
@@ -761,11 +819,21 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     for (int c = 0; c < kD / 4; ++c) po[c] = make_float4(0.f, 0.f, 0.f, 0.f);
                     a.part_lse[prow] = -INFINITY;
                 }
+                if (kScored && direct && valid) {          // (ranges that leave the whole row pair nothing)
+                    const int64_t row = ((int64_t)cb * nmax + tok) * a.H + kvh * a.G + gi;
+                    uint4 *po = reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.out) + row * (kD * (a.out_f32 ? 4 : 2)));
+#pragma unroll 4
+                    for (int c = 0; c < (a.out_f32 ? kD / 4 : kD / 8); ++c) po[c] = make_uint4(0u, 0u, 0u, 0u);
+                    if (a.lse) a.lse[row] = -INFINITY;
+                }
                 ok = pass_spare_turns();
                 continue;
             }
             float m_ref = -INFINITY;   // reference maximum (raw score units) the probabilities are scaled by
             float l = 0.f;
+            // (kScored) the head's slope in log2 units per row of distance
+            float slope = 0.f;
+            if (kScored && a.mods.slopes && valid) slope = a.mods.slopes[kvh * a.G + gi] * kLog2e;
             for (int j = j0, k = 0; j < ntiles; j += jstep, ++it, ++k) {
                 ok = mbar_wait(bar(B_SFULL0 + i), it & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
@@ -785,9 +853,9 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     continue;
                 }
                 const int64_t key0 = (int64_t)wt.actual(kt0 + j) * kRows;
-                const int nvis = (int)max((int64_t)0, min((int64_t)kRows, limit - key0));
+                const int nvis = (int)max((int64_t)0, min((int64_t)kRows, (kScored ? limit_s : limit) - key0));
                 // a tile that starts before the window holds hidden columns (the sink tile, the window's first)
-                const bool masked = key0 + kRows > clear || (kWindow && key0 < a.win_lo);
+                const bool masked = key0 + kRows > clear || (kWindow && key0 < a.win_lo) || (kScored && key0 < clear_from);
 
                 // the whole score row in registers after one load
                 uint32_t sc[128];
@@ -796,13 +864,71 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 KVF_TMEM_LD32(sc, 64, t_s + 64);
                 KVF_TMEM_LD32(sc, 96, t_s + 96);
                 tmem_wait_ld();
+                bool in_place = true;          // (kScored) the scores in sc are what the softmax takes; else small[] is yet to come
+                float m_small = 0.f;
+                if constexpr (kScored) {
+                    auto pair = [&](int c) { return make_float2(__uint_as_float(sc[c]), __uint_as_float(sc[c + 1])); };
+                    auto put = [&](int c, float2 x) { sc[c] = __float_as_uint(x.x); sc[c + 1] = __float_as_uint(x.y); };
+                    if (a.mods.cap_out > 0.f) {
+                        // what the tile's largest score in magnitude allows (rows past the chunk's end do not count)
+                        float hi[4], lo[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            hi[q] = fmaxf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
+                            lo[q] = fminf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
+                        }
+#pragma unroll
+                        for (int c = 8; c < 128; c += 8)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                hi[q] = max3(hi[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
+                                lo[q] = min3(lo[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
+                            }
+                        const float top = fmaxf(max3(hi[0], hi[1], hi[2]), hi[3]), low = fminf(min3(lo[0], lo[1], lo[2]), lo[3]);
+                        const float far = valid ? fmaxf(top, -low) : 0.f;
+                        if (!__any_sync(0xffffffffu, far > a.mods.small_to)) {
+                            if (!masked && !a.mods.slopes) {
+                                in_place = false;
+                                m_small = top * cap_small_over(a.mods, both(top)).x;
+                            } else {
+#pragma unroll
+                                for (int c = 0; c < 128; c += 2) put(c, __fmul2_rn(pair(c), cap_small_over(a.mods, pair(c))));
+                            }
+                        } else if (!__any_sync(0xffffffffu, far > a.mods.middle_to)) {
+#pragma unroll
+                            for (int c = 0; c < 128; c += 2) put(c, cap_middle(a.mods, pair(c)));
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(cap_any(a.mods, __uint_as_float(sc[c])));
+                        }
+                    } else {
+                        const float2 by = both(a.scale_log2);
+#pragma unroll
+                        for (int c = 0; c < 128; c += 2) put(c, __fmul2_rn(pair(c), by));
+                    }
+                    if (a.mods.slopes) {
+                        const int64_t behind = a.mods.pos0 + tok - key0;          // distance of the tile's first key
+                        const float at = (float)behind;
+                        if (__all_sync(0xffffffffu, !valid || behind >= kRows - 1)) {
+                            const float2 from = both(-slope * at), per = both(slope);
+#pragma unroll
+                            for (int c = 0; c < 128; c += 2) put(c, __fadd2_rn(pair(c), __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from)));
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(fmaf(-slope, fabsf(at - (float)c), __uint_as_float(sc[c])));
+                        }
+                    }
+                }
                 if (masked) {
                     // columns below lo_c lie before the window and count only if they are sinks
-                    const int lo_c = kWindow ? (int)max((int64_t)0, min((int64_t)kRows, a.win_lo - key0)) : 0;
+                    const int lo_c = kWindow ? (int)max((int64_t)0, min((int64_t)kRows, a.win_lo - key0))
+                                   : kScored ? (int)max((int64_t)0, min((int64_t)kRows, begin_s - key0)) : 0;
                     const int sink_c = kWindow ? (int)max((int64_t)0, min((int64_t)kRows, a.n_sink - key0)) : 0;
 #pragma unroll
                     for (int c = 0; c < 128; ++c) sc[c] = (c < nvis && (c >= lo_c || c < sink_c)) ? sc[c] : 0xFF800000u;   // -inf
                 }
+                float m_tile = m_small;
+                if (!kScored || in_place) {
                 float mx[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) mx[q] = fmaxf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
@@ -811,7 +937,8 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         mx[q] = max3(mx[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
-                const float m_tile = fmaxf(max3(mx[0], mx[1], mx[2]), max3(max3(mx[3], mx[4], mx[5]), mx[6], mx[7]));
+                m_tile = fmaxf(max3(mx[0], mx[1], mx[2]), max3(max3(mx[3], mx[4], mx[5]), mx[6], mx[7]));
+                }
                 // move the reference only when the maximum grew by more than the threshold: the
                 // probabilities then stay below 2^threshold and the accumulator is rarely rescaled
                 const bool grow = (m_tile - m_ref) * sl2 > kRescaleThreshold;   // also true when m_ref = -inf < m_tile
@@ -858,7 +985,8 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
 
                 // probabilities; the first 64 keys are handed over before the rest is computed
                 uint32_t p[32];
-                exp_half(sc, p, sl2v, negv, acc0, acc1);
+                if (kScored && !in_place) exp_half_small(a.mods, sc, p, negv, acc0, acc1);
+                else exp_half(sc, p, sl2v, negv, acc0, acc1);
                 KVF_TMEM_ST32(p, 0, t_s);
                 tmem_wait_st();
                 tc_fence_before();
@@ -868,7 +996,8 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 // takes ~250 cycles to come even if it is yes; every phase is waited for)
                 uint32_t panel_free = 1;
                 if (kEarly && k > 0) panel_free = mbar_test(bar(B_PVDONE0 + i), (it - 1) & 1);
-                exp_half(sc + 64, p, sl2v, negv, acc0, acc1);
+                if (kScored && !in_place) exp_half_small(a.mods, sc + 64, p, negv, acc0, acc1);
+                else exp_half(sc + 64, p, sl2v, negv, acc0, acc1);
                 if (kEarly) {
                     if (!__all_sync(0xffffffffu, panel_free)) ok = wait_pv();
                     if (!ok) break;
@@ -1466,6 +1595,8 @@ int attn_tc_row_ranks(int units, int sms, int64_t key_tiles) {
     return units <= sms && key_tiles <= 46 * (int64_t)units / sms - 10 ? 1 : 0;
 }
 
+void set_score_cap(ScoreMods &m, double scale, double softcap) { set_cap(m, scale, softcap); }
+
 cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s) {
     static_assert(sizeof(Ctl) <= 512, "control block");
     static_assert(kSmemBytes <= 232448, "shared memory budget of one CTA");
@@ -1474,6 +1605,7 @@ cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     const bool quant = a.quant_bits != 0;
     auto kernel = a.quant_bits == 8 ? (a.win_lo > 0 ? attn_tc_kernel<true, 8, false, false> : attn_tc_kernel<false, 8, false, false>)
                 : a.quant_bits == 4 ? (a.win_lo > 0 ? attn_tc_kernel<true, 4, false, false> : attn_tc_kernel<false, 4, false, false>)
+                : a.scored          ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, true> : attn_tc_kernel<false, 0, false, false, 0, true>)
                                     : a.streams == 1      ? (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, true> : attn_tc_kernel<false, 0, false, true>)
                                     : (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, false> : attn_tc_kernel<false, 0, false, false>);
     const uint32_t smem = quant ? kSmemBytesQ8 : kSmemBytes;

@@ -325,18 +325,18 @@ int64_t window_lo(const kvf_cache *c, int64_t prefix) {
 }
 
 // (`ragged`: the members' row counts are known on the device only, and with them which ranges a KV head has)
-// (`scored`: capped, biased or range-masked scores - not in one launch, and on the CUDA cores)
+// (`scored`: capped, biased or range-masked scores - not in one launch, and fp32 rows on the CUDA cores)
 Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t part_rows_cap = -1, bool one_launch = true, bool ragged = false,
                bool scored = false) {
     if (part_rows_cap < 0) part_rows_cap = c->part_rows_cap;
     Plan p;
     p.qdec = p.small = false;
-    p.tc = (c->tc || c->tc32) && !scored;
+    p.tc = c->tc || (c->tc32 && !scored);
     one_launch = one_launch && !scored;
     p.ngroups = p.ranks = 0;
     const int64_t L = prefix + n;
     const int Hkv = c->cfg.n_kv_heads;
-    if ((c->quant || c->tc) && !scored && c->window <= 0 && n * c->G <= attn_q8_decode_max_rows()) {
+    if ((c->quant || c->tc) && c->window <= 0 && n * c->G <= attn_q8_decode_max_rows()) {
         // one CTA per SM (all caches of a batch together), each inside one KV head (a multiple of the KV heads),
         // at least two key tiles each; a forced split count is the number of ranges per KV head
         const int64_t nt = (L + kKvTile - 1) / kKvTile;
@@ -656,10 +656,7 @@ ScoreMods score_mods(const kvf_cache *c, const kvf_scores *sc, int64_t pos0) {
     ScoreMods m = {};
     m.pos0 = pos0;
     if (!sc) return m;
-    if (sc->softcap > 0.0) {
-        m.cap_in = (float)(c->scale_log2 * 0.6931471805599453 / sc->softcap);
-        m.cap_out = (float)(sc->softcap * 1.4426950408889634);
-    }
+    if (sc->softcap > 0.0) set_score_cap(m, c->scale_log2 * 0.6931471805599453, sc->softcap);
     m.slopes = sc->slopes;
     m.first = sc->first;
     m.end = sc->end;
@@ -765,7 +762,7 @@ kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void 
         ProfScope ps(c, st, 1);
         if (plan.small) e = launch_fold_small(ra, aa, plan.cut, f.dtype, (f.flags & KVF_ROPE_INTERLEAVED) != 0, st);
         else if (plan.qdec) e = launch_attn_q8_decode(aa, c->maps, st);
-        else if (plan.tc && c->tc) e = launch_attn_tc(aa, c->maps, st);
+        else if (c->tc) e = launch_attn_tc(aa, c->maps, st);
         else if (plan.tc) e = launch_attn_tc32(aa, st);
         else e = launch_attn_simt(aa, f.dtype, st, nullptr);
     }
@@ -869,7 +866,7 @@ kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
     if ((sc->slopes && check_f32(sc->slopes)) || (sc->first && check_f32(reinterpret_cast<const float *>(sc->first))) ||
         (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
         return KVF_ERR_INVALID_ARG;
-    if (c->window > 0 || c->quant || c->page_table) return KVF_ERR_UNSUPPORTED;
+    if (c->window > 0 || c->quant) return KVF_ERR_UNSUPPORTED;
     return KVF_OK;
 }
 

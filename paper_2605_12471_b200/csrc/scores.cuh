@@ -21,5 +21,43 @@ __device__ __forceinline__ RowRange seen_rows(const ScoreMods &m, int64_t at, in
     return r;
 }
 
+// The cap, softcap * log2(e) * tanh(x) with x = scale / softcap * (q . k).  The special-function unit is what a softmax on the tensor
+// cores is short of, so that most scores go through multiply-adds: tanh(x) / x as a polynomial in x^2, of least relative error
+// over |x| <= 0.2 (three terms, 1.1e-7) and |x| <= 0.75 (five, 5.7e-7); coefficients by the exchange algorithm of Remez.  Beyond,
+// and where one score of a warp's tile lies there, 1 - 2 / (1 + e^2x), whose error of 2^-22 is one of the cap.
+constexpr float kSmallX = 0.2f, kMiddleX = 0.75f;
+constexpr double kSmallTanh[3] = {0.9999998947912137, -0.33328590898391885, 0.13015407544114974};
+constexpr double kMiddleTanh[5] = {0.9999994349238549, -0.33328251532272035, 0.13258983219087364, -0.050056302629619055, 0.012929632363192806};
+inline void set_cap(ScoreMods &m, double scale, double softcap) {
+    const double in = scale / softcap, out = softcap * 1.4426950408889634;
+    m.cap_in = (float)in;
+    m.cap_out = (float)out;
+    // (powers of `in` below fp32's range, under caps of a million and more: the middle polynomial alone, which does without)
+    m.small_to = in > 1e-7 ? (float)(kSmallX / in) : 0.f;
+    for (int i = 0; i < 3; ++i) m.small[i] = (float)(kSmallTanh[i] * out * in * (i > 0 ? in * in : 1.0) * (i > 1 ? in * in : 1.0));
+    m.middle_to = (float)(kMiddleX / in);
+    for (int i = 0; i < 5; ++i) m.middle[i] = (float)(kMiddleTanh[i] * out);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 cap_middle(const ScoreMods &m, float2 s) {
+    const float2 x = __fmul2_rn(s, both(m.cap_in)), u = __fmul2_rn(x, x);
+    float2 y = __ffma2_rn(u, both(m.middle[4]), both(m.middle[3]));
+    y = __ffma2_rn(u, y, both(m.middle[2]));
+    y = __ffma2_rn(u, y, both(m.middle[1]));
+    y = __ffma2_rn(u, y, both(m.middle[0]));
+    return __fmul2_rn(x, y);
+}
+// (s * cap_small_over is the score)
+__device__ __forceinline__ float2 cap_small_over(const ScoreMods &m, float2 s) {
+    const float2 u = __fmul2_rn(s, s);
+    return __ffma2_rn(u, __ffma2_rn(u, both(m.small[2]), both(m.small[1])), both(m.small[0]));
+}
+__device__ __forceinline__ float cap_any(const ScoreMods &m, float s) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * (m.cap_in * (2.f * kLog2e))));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return m.cap_out * fmaf(-2.f, r, 1.f);
+}
+
 }  // namespace
 }  // namespace kvf
