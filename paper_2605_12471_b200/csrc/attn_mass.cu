@@ -3,11 +3,341 @@
 // s_ihr = scale * q_ih . k_gr, capped and biased as in a scored step, lse the softmax denominators that the step left.  (The paper prunes
 // by attention weight in its Discussion and gives no scheme; this is the quantity that such schemes add up.)  It is the
 // attention without its values: no running maximum, because the denominators are known, and sums over queries, not over keys.
+//
+// bf16 rows run on the tensor cores.  A tile is S^T = K Q^T, 128 keys of one KV head by up to 128 query rows (whole tokens of its G
+// query heads), so that a thread has one key's row of tensor memory and the sum over queries is its own: what would be a reduction
+// over lanes in the attention kernels costs nothing here.  Per (KV head, key tile) the K tile stays in shared memory while the query
+// tiles come by (L2 holds them); where the chunk is one query tile that one stays and the keys stream.  Jobs (one query tile
+// against one key tile) go to two groups of four warps in turn, four accumulators of 128 columns deep.
+// What bounds it: one exponential per score, 1024 cycles of the special-function unit for a tile whose MMAs take 512; a decoded token is
+// bound by the K plane's bytes.
 #include "kvfold_internal.h"
+#include "sm100_ptx.cuh"
 #include "scores.cuh"
 
 namespace kvf {
 namespace {
+
+// ---- tensor cores
+constexpr int kTile = 128, kD = 128;
+constexpr uint32_t kPanel = 128 * 128, kTileBytes = 2 * kPanel;
+constexpr int kTcThreads = 384;                // warp 0 TMA, warp 1 MMA (2 and 3 idle), warps 4 - 11 exponentials
+constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: two K slots, four Q slots; one: five and one
+constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory
+constexpr uint32_t kTmemCols = 512;
+struct Col {
+    float neg;                                 // -lse * log2(e) of the query row (-inf: no such row, or it saw nothing)
+    uint32_t seen;                             // keys of the tile that it sees, [low half, high half)
+    float slope, at;                           // slope in log2 units, its distance to the tile's first key
+};
+enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + kAccs,
+       M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_COUNT };
+struct MassCtl {
+    unsigned long long bars[M_COUNT];
+    uint32_t tmem_base;
+    int abort;
+    float sums[kTile];                         // the second group's sums on their way to the first
+};
+constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // 128 columns for each of the eight warps
+constexpr uint32_t kOffMassCtl = kOffCols + 8 * kTile * sizeof(Col);
+constexpr uint32_t kMassSmem = kOffMassCtl + 1024 + 1024;
+static_assert(sizeof(MassCtl) <= 1024 && kMassSmem <= 232448, "shared memory budget of one CTA");
+
+__device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// What the roles have to agree on.  Item = (KV head, key tile, split of the query tiles); its jobs are query tiles [q0, q1).
+struct MassWork {
+    int nkt, nq, toks, splits, one;            // key tiles of a KV head, query tiles, tokens of a query tile
+    int64_t items;                             // (below 2^31)
+    __device__ __forceinline__ void item(const MassArgs &a, int64_t i, int &kvh, int &kt, int &split, int &q0, int &q1) const {
+        const uint32_t u = (uint32_t)i / (uint32_t)splits;
+        split = (int)((uint32_t)i - u * (uint32_t)splits);
+        kvh = (int)(u / (uint32_t)nkt);
+        kt = (int)u - kvh * nkt;
+        // (without ranges, tokens whose row lies below the key tile see none of it)
+        const int64_t ahead = (int64_t)kt * kTile - (a.rows - a.n);
+        int from = 0;
+        if (a.self_rows && !(a.scored && (a.mods.first || a.mods.end)) && ahead > 0) from = (int)(ahead / toks);
+        q0 = from + (int)((int64_t)split * (nq - from) / splits);
+        q1 = from + (int)((int64_t)(split + 1) * (nq - from) / splits);
+    }
+};
+
+// kOne: the chunk is one query tile of `ncols` columns (a multiple of 16).
+template <bool kOne>
+__global__ void __launch_bounds__(kTcThreads, 1)
+mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
+    constexpr int SK = kOne ? 5 : 2, SQ = kOne ? 1 : 4;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - smem_u32(smem_raw));
+    MassCtl *ctl = reinterpret_cast<MassCtl *>(smem + kOffMassCtl);
+    auto bar = [&](int i) { return base + kOffMassCtl + 8u * (uint32_t)i; };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t L = a.rows, P = L - (int64_t)a.n * a.self_rows;
+    const int G = a.G;
+    // items of this CTA: a contiguous range of them (kOne: the K rows of one stretch), else every gridDim-th
+    const int64_t i0 = kOne ? blockIdx.x * w.items / gridDim.x : blockIdx.x, i1 = kOne ? (blockIdx.x + 1) * w.items / gridDim.x : w.items;
+    const int64_t istep = kOne ? 1 : gridDim.x;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < SK; ++s) { mbar_init(bar(M_KFULL + s), 1); mbar_init(bar(M_KEMPTY + s), 1); }
+        for (int s = 0; s < SQ; ++s) { mbar_init(bar(M_QFULL + s), 1); mbar_init(bar(M_QEMPTY + s), 1); }
+        for (int s = 0; s < kAccs; ++s) { mbar_init(bar(M_DFULL + s), 1); mbar_init(bar(M_DEMPTY + s), 4); }
+        for (int s = 0; s < 4; ++s) { mbar_init(bar(M_SUM + s), 1); mbar_init(bar(M_TAKEN + s), 1); }
+        mbar_init(bar(M_DRAIN), 1);
+        ctl->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    {
+        // rows of a query tile behind its last token (G does not divide 128), which no copy fills
+        const int from = w.toks * G * 128, bytes = (int)kPanel - from;
+        for (int i = threadIdx.x * 16; i < 2 * SQ * bytes; i += kTcThreads * 16)
+            *reinterpret_cast<uint4 *>(smem + (uint32_t)SK * kTileBytes + (uint32_t)(i / bytes) * kPanel + from + i % bytes) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    pdl_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();          // nothing above reads what an earlier kernel wrote
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&ctl->tmem_base);
+    auto k_slot = [&](int s) { return base + (uint32_t)s * kTileBytes; };
+    auto q_slot = [&](int s) { return base + (uint32_t)(SK + s) * kTileBytes; };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ------------------------------------------------------------------ TMA producer
+            const uint32_t q_bytes = 2u * (uint32_t)(w.toks * G) * 128u;
+            int kc = 0, qc = 0, held = -1;       // tiles loaded so far; kOne: KV head of the query tile held
+            bool ok = true;
+            for (int64_t i = i0; ok && i < i1; i += istep) {
+                int kvh, kt, split, q0, q1;
+                w.item(a, i, kvh, kt, split, q0, q1);
+                if (q0 >= q1) continue;
+                ok = mbar_wait(bar(M_KEMPTY + kc % SK), ((kc / SK) & 1) ^ 1, ctl, a.status);
+                if (!ok) break;
+                const uint32_t kb = bar(M_KFULL + kc % SK), kd = k_slot(kc % SK);
+                mbar_expect_tx(kb, kTileBytes);
+                if (a.page_table) {
+                    const int page = a.page_table[kt];
+                    tma_load_4d(kd, &map_k, kb, 0, 0, kvh, page);
+                    tma_load_4d(kd + kPanel, &map_k, kb, 64, 0, kvh, page);
+                } else {
+                    tma_load_3d(kd, &map_k, kb, 0, kt * kTile, kvh);
+                    tma_load_3d(kd + kPanel, &map_k, kb, 64, kt * kTile, kvh);
+                }
+                ++kc;
+                for (int q = q0; q < q1; ++q) {
+                    if (kOne && held == kvh) break;
+                    held = kvh;
+                    ok = mbar_wait(bar(M_QEMPTY + qc % SQ), ((qc / SQ) & 1) ^ 1, ctl, a.status);
+                    if (!ok) break;
+                    const uint32_t qb = bar(M_QFULL + qc % SQ), qd = q_slot(qc % SQ);
+                    mbar_expect_tx(qb, q_bytes);
+                    tma_load_3d(qd, &map_q, qb, 0, kvh * G, q * w.toks);
+                    tma_load_3d(qd + kPanel, &map_q, qb, 64, kvh * G, q * w.toks);
+                    ++qc;
+                }
+            }
+            // do not leave while a copy may still be writing into this CTA's shared memory
+            for (int c = max(0, kc - SK); c < kc; ++c) mbar_wait_drain(bar(M_KFULL + c % SK), (c / SK) & 1, a.status);
+            for (int c = max(0, qc - SQ); c < qc; ++c) mbar_wait_drain(bar(M_QFULL + c % SQ), (c / SQ) & 1, a.status);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer: the warp walks the loop, one thread of it issues
+        const bool leader = elect_one();
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(ncols >> 3) << 17) | ((128u >> 4) << 24);
+        int kc = 0, qc = 0, jc = 0, held = -1;
+        bool ok = true;
+        for (int64_t i = i0; ok && i < i1; i += istep) {
+            int kvh, kt, split, q0, q1;
+            w.item(a, i, kvh, kt, split, q0, q1);
+            if (q0 >= q1) continue;
+            if (kOne && held >= 0 && held != kvh) {          // the last head's query tile has been read
+                if (leader) tc_commit(bar(M_QEMPTY));
+                ++qc;
+            }
+            ok = mbar_wait_warp(bar(M_KFULL + kc % SK), (kc / SK) & 1, ctl, a.status);
+            if (!ok) break;
+            const uint64_t kdesc = desc_kmajor(k_slot(kc % SK));
+            for (int q = q0; q < q1; ++q, ++jc) {
+                if (!kOne || held != kvh) ok = mbar_wait_warp(bar(M_QFULL + qc % SQ), (qc / SQ) & 1, ctl, a.status);
+                held = kvh;
+                if (ok) ok = mbar_wait_warp(bar(M_DEMPTY + jc % kAccs), ((jc / kAccs) & 1) ^ 1, ctl, a.status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t qdesc = desc_kmajor(q_slot(qc % SQ));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    const uint64_t off = (uint64_t)(((kk >> 2) * kPanel + (kk & 3) * 32) >> 4);
+                    if (leader) tc_mma(tmem + (uint32_t)(jc % kAccs) * 128u, kdesc + off, qdesc + off, idesc, kk > 0);
+                }
+                if (leader) tc_commit(bar(M_DFULL + jc % kAccs));
+                if (!kOne) {
+                    if (leader) tc_commit(bar(M_QEMPTY + qc % SQ));
+                    ++qc;
+                }
+            }
+            if (!ok) break;
+            if (leader) tc_commit(bar(M_KEMPTY + kc % SK));
+            ++kc;
+        }
+        // whatever made this warp leave its loop, tensor memory is released only after every MMA it issued has run
+        if (leader) {
+            tc_commit(bar(M_DRAIN));
+            mbar_wait_drain(bar(M_DRAIN), 0, a.status);
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ exponentials: a thread per key
+        const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t cols = base + kOffCols + (uint32_t)(warp - 4) * (kTile * (uint32_t)sizeof(Col));
+        Col *mine = reinterpret_cast<Col *>(smem + kOffCols) + (warp - 4) * kTile;
+        const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
+        const float2 sl2 = both(a.scale_log2);
+        int jc = 0, sums = 0;
+        bool ok = true;
+        for (int64_t i = i0; ok && i < i1; i += istep) {
+            int kvh, kt, split, q0, q1;
+            w.item(a, i, kvh, kt, split, q0, q1);
+            const int64_t key0 = (int64_t)kt * kTile;
+            float2 acc0 = both(0.f), acc1 = both(0.f);
+            const int jc0 = jc;
+            for (int q = q0; q < q1; ++q, ++jc) {
+                if ((jc & 1) != group) continue;
+                // the query rows of the tile, four a lane
+                bool some = false, part = false;
+                __syncwarp();                    // (the last job's are read)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = lane + 32 * k, tok = q * w.toks + c / G, h = kvh * G + c % G;
+                    Col x = {-INFINITY, 0u, 0.f, 0.f};
+                    if (c >= w.toks * G) {
+                        // (zeros)
+                    } else if (tok >= a.n) {
+                        part = true;
+                    } else {
+                        const RowRange seen = a.scored ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, P + (int64_t)(tok + 1) * a.self_rows};
+                        const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kTile), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kTile);
+                        if (lo < hi) {
+                            const float l = a.lse[(int64_t)tok * a.H + h];
+                            x.neg = l == -INFINITY ? -INFINITY : -l * kLog2e;
+                            x.seen = (uint32_t)lo | (uint32_t)hi << 16;
+                            if (biased) {
+                                x.slope = a.mods.slopes[h] * kLog2e;
+                                x.at = (float)(a.mods.pos0 + tok - key0);
+                            }
+                            some = true;
+                        }
+                        part = part || lo > 0 || hi < kTile;
+                    }
+                    mine[c] = x;
+                }
+                some = __any_sync(0xffffffffu, some);
+                part = __any_sync(0xffffffffu, part);
+                __syncwarp();
+                ok = mbar_wait(bar(M_DFULL + jc % kAccs), (jc / kAccs) & 1, ctl, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t t_job = t_acc + (uint32_t)(jc % kAccs) * 128u;
+#pragma unroll 1
+                for (int c0 = 0; some && c0 < ncols; c0 += 16) {
+                    uint32_t v[16];
+                    KVF_TMEM_LD16(v, 0, t_job + c0);
+                    tmem_wait_ld();
+                    float2 x[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) x[c] = make_float2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                    if (cap) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) x[c] = make_float2(cap_any(a.mods, x[c].x), cap_any(a.mods, x[c].y));
+                    }
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        Col p, q2;
+                        const uint32_t at = cols + (uint32_t)(c0 + 2 * c) * (uint32_t)sizeof(Col);
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=f"(p.neg), "=r"(p.seen), "=f"(p.slope), "=f"(p.at) : "r"(at));
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=f"(q2.neg), "=r"(q2.seen), "=f"(q2.slope), "=f"(q2.at) : "r"(at + 16u));
+                        float2 y = cap ? __fadd2_rn(x[c], make_float2(p.neg, q2.neg)) : __ffma2_rn(x[c], sl2, make_float2(p.neg, q2.neg));
+                        if (biased) {
+                            y.x = fmaf(-p.slope, fabsf(p.at - (float)r), y.x);
+                            y.y = fmaf(-q2.slope, fabsf(q2.at - (float)r), y.y);
+                        }
+                        if (part) {
+                            y.x = r >= (int)(p.seen & 0xFFFFu) && r < (int)(p.seen >> 16) ? y.x : -INFINITY;
+                            y.y = r >= (int)(q2.seen & 0xFFFFu) && r < (int)(q2.seen >> 16) ? y.y : -INFINITY;
+                        }
+                        const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                        if (c & 1) acc1 = __fadd2_rn(acc1, e);
+                        else acc0 = __fadd2_rn(acc0, e);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(M_DEMPTY + jc % kAccs));
+            }
+            if (!ok) break;
+            const float2 acc = __fadd2_rn(acc0, acc1);
+            float sum = acc.x + acc.y;
+            if (kOne) {
+                if (jc == jc0 ? group != 0 : (jc0 & 1) != group) continue;           // the other group had the job
+            } else {
+                // the second group's sum of the key goes to the first
+                ++sums;
+                if (group == 1) {
+                    if (sums > 1) ok = mbar_wait(bar(M_TAKEN + quarter), (sums - 2) & 1, ctl, a.status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    *reinterpret_cast<volatile float *>(&ctl->sums[r]) = sum;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(M_SUM + quarter));
+                    continue;
+                }
+                ok = mbar_wait(bar(M_SUM + quarter), (sums - 1) & 1, ctl, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                sum += *reinterpret_cast<volatile float *>(&ctl->sums[r]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(M_TAKEN + quarter));
+            }
+            const int64_t key = key0 + r;
+            if (key >= L) continue;
+            if (w.splits > 1) {
+                a.parts[((int64_t)split * a.Hkv + kvh) * L + key] = sum;
+            } else {
+                if (a.mass_in && a.decay != 0.f && key < a.held) sum = fmaf(a.decay, a.mass_in[(int64_t)kvh * a.in_stride + key], sum);
+                a.mass_out[(int64_t)kvh * a.out_stride + key] = sum;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+// The splits' sums of a key, in order.
+__global__ void __launch_bounds__(256) mass_sum_kernel(const MassArgs a, const int splits) {
+    const int64_t key = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int kvh = blockIdx.y;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (key >= a.rows) return;
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s) sum += a.parts[((int64_t)s * a.Hkv + kvh) * a.rows + key];
+    if (a.mass_in && a.decay != 0.f && key < a.held) sum = fmaf(a.decay, a.mass_in[(int64_t)kvh * a.in_stride + key], sum);
+    a.mass_out[(int64_t)kvh * a.out_stride + key] = sum;
+}
 
 // ---- CUDA cores (fp32 caches, head_dim 64): 64 keys of one KV head a CTA, the query rows in tiles of 64, as attn_simt.cu has them
 constexpr int BM = 64, BN = 64, kThreads = 256;
@@ -135,6 +465,34 @@ cudaError_t launch_simt_t(const MassArgs &a, cudaStream_t s) {
 }
 
 }  // namespace
+
+int mass_tile_tokens(int G) { return kTile / G; }
+
+cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CUtensorMap &map_k, cudaStream_t s) {
+    MassWork w;
+    w.toks = mass_tile_tokens(a.G);
+    w.nkt = (int)((a.rows + kTile - 1) / kTile);
+    w.nq = (a.n + w.toks - 1) / w.toks;
+    w.one = w.nq == 1;
+    const int64_t units = (int64_t)a.Hkv * w.nkt;
+    // Splits of the query tiles: as many as fill the waves of CTAs best (a fifth of a tile for what an item costs besides)
+    w.splits = 1;
+    double least = 0.0;
+    for (int sp = 1; sp <= w.nq && sp <= 8 && (int64_t)sp * a.Hkv * a.rows <= a.parts_cap; ++sp) {
+        const double waves = (double)((units * sp + a.sms - 1) / a.sms), t = waves * ((double)w.nq / sp + 0.2) + (sp > 1 ? 2.0 : 0.0);
+        if (sp == 1 || t < least) { least = t; w.splits = sp; }
+    }
+    w.items = units * w.splits;
+    if (w.items >= (int64_t)1 << 31) return cudaErrorInvalidValue;          // (2^24 tiles of 128 rows for each of 16 heads, and beyond)
+    const int ncols = w.one ? (a.n * a.G + 15) / 16 * 16 : kTile;
+    auto kernel = w.one ? mass_tc_kernel<true> : mass_tc_kernel<false>;
+    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(kernel), (int)kMassSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t ctas = w.items < a.sms ? w.items : a.sms;
+    e = launch_pdl(kernel, dim3((unsigned)ctas), dim3(kTcThreads), kMassSmem, s, a, w, ncols, map_q, map_k);
+    if (e != cudaSuccess || w.splits == 1) return e;
+    return launch_pdl(mass_sum_kernel, dim3((unsigned)((a.rows + 255) / 256), a.Hkv), dim3(256), 0, s, a, w.splits);
+}
 
 cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s) {
     if (dtype == 0) return a.d == 128 ? launch_simt_t<__nv_bfloat16, 128>(a, s) : launch_simt_t<__nv_bfloat16, 64>(a, s);

@@ -1094,7 +1094,7 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0 || c->len < 1 || (appended != 0 && appended != 1)) return KVF_ERR_INVALID_ARG;
     if (appended && n_tokens > c->len) return KVF_ERR_INVALID_ARG;
     if (!std::isfinite(decay)) return KVF_ERR_INVALID_ARG;
-    if (c->quant || c->page_table || c->window > 0) return KVF_ERR_UNSUPPORTED;
+    if (c->quant || c->window > 0) return KVF_ERR_UNSUPPORTED;
     if (scores) {
         const kvf_status s = check_scores(c, scores);
         if (s != KVF_OK) return s;
@@ -1125,8 +1125,24 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     a.scored = scores != nullptr;
     a.mods = score_mods(c, scores, pos0);
     a.sms = c->sm_count;
+    // (the set of partial results that the next step writes: an open merge may still be reading the other)
+    a.parts = reinterpret_cast<float *>(c->workspace + (c->comb_stream && c->part_set == 1 ? c->lay.part_o2 : c->lay.part_o));
+    a.parts_cap = c->part_rows_cap * f.head_dim;
     const PdlScope pdl(dependent_launches());
-    const cudaError_t e = launch_mass_simt(a, f.dtype, static_cast<cudaStream_t>(cuda_stream));
+    cudaError_t e;
+    if (c->tc) {
+        EncodeTiledFn fn = nullptr;
+        kvf_status s = encode_fn(&fn);
+        if (s != KVF_OK) return s;
+        CUtensorMap map_q;
+        const uint64_t row = (uint64_t)f.head_dim * 2;
+        s = make_map(fn, &map_q, const_cast<void *>(q_rot), (uint64_t)f.n_q_heads, (uint64_t)n_tokens, row, row * f.n_q_heads, f.head_dim,
+                     (uint32_t)c->G, (uint32_t)mass_tile_tokens(c->G));
+        if (s != KVF_OK) return s;
+        e = launch_mass_tc(a, map_q, c->maps.k, static_cast<cudaStream_t>(cuda_stream));
+    } else {
+        e = launch_mass_simt(a, f.dtype, static_cast<cudaStream_t>(cuda_stream));
+    }
     if (e != cudaSuccess) return cuda_fail(e, "mass launch");
     c->launches++;
     return KVF_OK;
