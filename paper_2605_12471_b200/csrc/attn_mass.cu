@@ -11,6 +11,8 @@
 // against one key tile) go to two groups of four warps in turn, four accumulators of 128 columns deep.
 // What bounds it: one exponential per score, 1024 cycles of the special-function unit for a tile whose MMAs take 512; a decoded token is
 // bound by the K plane's bytes.
+#include <type_traits>
+
 #include "kvfold_internal.h"
 #include "sm100_ptx.cuh"
 #include "scores.cuh"
@@ -25,10 +27,10 @@ constexpr int kTcThreads = 384;                // warp 0 TMA, warp 1 MMA (2 and 
 constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: two K slots, four Q slots; one: five and one
 constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory
 constexpr uint32_t kTmemCols = 512;
-struct Col {
-    float neg;                                 // -lse * log2(e) of the query row (-inf: no such row, or it saw nothing)
-    uint32_t seen;                             // keys of the tile that it sees, [low half, high half)
-    float slope, at;                           // slope in log2 units, its distance to the tile's first key
+struct __align__(16) Cols {                    // what a warp knows of a job's columns (query rows)
+    float neg[kTile];                          // -lse * log2(e) (-inf: no such row, or it saw nothing)
+    uint32_t seen[kTile];                      // keys of the tile that it sees, [low half, high half); filled where some may not be
+    float2 bias[kTile];                        // slope in log2 units, distance of the tile's first key; filled under slopes
 };
 enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + kAccs,
        M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_COUNT };
@@ -38,8 +40,8 @@ struct MassCtl {
     int abort;
     float sums[kTile];                         // the second group's sums on their way to the first
 };
-constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // 128 columns for each of the eight warps
-constexpr uint32_t kOffMassCtl = kOffCols + 8 * kTile * sizeof(Col);
+constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // for each of the eight warps
+constexpr uint32_t kOffMassCtl = kOffCols + 8 * sizeof(Cols);
 constexpr uint32_t kMassSmem = kOffMassCtl + 1024 + 1024;
 static_assert(sizeof(MassCtl) <= 1024 && kMassSmem <= 232448, "shared memory budget of one CTA");
 
@@ -198,11 +200,49 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         // ------------------------------------------------------------------ exponentials: a thread per key
         const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t cols = base + kOffCols + (uint32_t)(warp - 4) * (kTile * (uint32_t)sizeof(Col));
-        Col *mine = reinterpret_cast<Col *>(smem + kOffCols) + (warp - 4) * kTile;
+        Cols *mine = reinterpret_cast<Cols *>(smem + kOffCols) + (warp - 4);
+        const uint32_t neg = smem_u32(mine->neg);
         const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
+        const bool ranged = a.scored && (a.mods.first || a.mods.end);
         const float2 sl2 = both(a.scale_log2);
-        int jc = 0, sums = 0;
+        // my four columns of a query tile: 32 apart, token and head within the group
+        int tok_of[4], head_of[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            tok_of[k] = (lane + 32 * k) / G;
+            head_of[k] = (lane + 32 * k) % G;
+        }
+        // denominators of a query tile, as they enter an exponent
+        auto load_neg = [&](int kvh, int q, float (&l)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int tok = q * w.toks + tok_of[k];
+                l[k] = tok_of[k] < w.toks && tok < a.n ? a.lse[(int64_t)tok * a.H + kvh * G + head_of[k]] : -INFINITY;
+            }
+        };
+        auto put_neg = [&](const float (&l)[4]) {
+            __syncwarp();                        // (the last ones are read)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mine->neg[lane + 32 * k] = l[k] == -INFINITY ? -INFINITY : -l[k] * kLog2e;
+            __syncwarp();
+        };
+        // My jobs' query tiles one ahead: the denominators come from memory while the job before is worked on.
+        float ahead[4];
+        int64_t ai = i0 - istep;
+        int aq = 0, aq1 = 0, aj = -1, akvh = 0, akt, asplit;
+        auto look_ahead = [&]() {
+            do {
+                ++aq;
+                while (aq >= aq1 && ai < i1) {
+                    ai += istep;
+                    if (ai < i1) w.item(a, ai, akvh, akt, asplit, aq, aq1);
+                }
+                ++aj;
+            } while (ai < i1 && (aj & 1) != group);
+            if (ai < i1) load_neg(akvh, aq, ahead);
+        };
+        if (!kOne) look_ahead();
+        int jc = 0, sums = 0, held = -1;
         bool ok = true;
         for (int64_t i = i0; ok && i < i1; i += istep) {
             int kvh, kt, split, q0, q1;
@@ -212,72 +252,122 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             const int jc0 = jc;
             for (int q = q0; q < q1; ++q, ++jc) {
                 if ((jc & 1) != group) continue;
-                // the query rows of the tile, four a lane
-                bool some = false, part = false;
-                __syncwarp();                    // (the last job's are read)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int c = lane + 32 * k, tok = q * w.toks + c / G, h = kvh * G + c % G;
-                    Col x = {-INFINITY, 0u, 0.f, 0.f};
-                    if (c >= w.toks * G) {
-                        // (zeros)
-                    } else if (tok >= a.n) {
-                        part = true;
-                    } else {
-                        const RowRange seen = a.scored ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, P + (int64_t)(tok + 1) * a.self_rows};
-                        const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kTile), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kTile);
-                        if (lo < hi) {
-                            const float l = a.lse[(int64_t)tok * a.H + h];
-                            x.neg = l == -INFINITY ? -INFINITY : -l * kLog2e;
-                            x.seen = (uint32_t)lo | (uint32_t)hi << 16;
-                            if (biased) {
-                                x.slope = a.mods.slopes[h] * kLog2e;
-                                x.at = (float)(a.mods.pos0 + tok - key0);
-                            }
-                            some = true;
-                        }
-                        part = part || lo > 0 || hi < kTile;
-                    }
-                    mine[c] = x;
+                if (!kOne) {
+                    put_neg(ahead);
+                    look_ahead();
+                } else if (held != kvh) {
+                    load_neg(kvh, q, ahead);
+                    put_neg(ahead);
+                    held = kvh;
                 }
-                some = __any_sync(0xffffffffu, some);
-                part = __any_sync(0xffffffffu, part);
-                __syncwarp();
+                // does every token see all of the key tile?  (without ranges known from the tile's first token)
+                bool some = true, part = ranged || key0 + kTile > P + (int64_t)(q * w.toks + 1) * a.self_rows;
+                if (part || biased) {
+                    some = part = false;
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int tok = q * w.toks + tok_of[k];
+                        uint32_t sees = 0u;
+                        float2 bias = both(0.f);
+                        if (tok_of[k] < w.toks && tok < a.n) {
+                            const RowRange seen = a.scored ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, P + (int64_t)(tok + 1) * a.self_rows};
+                            const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kTile), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kTile);
+                            if (lo < hi) {
+                                sees = (uint32_t)lo | (uint32_t)hi << 16;
+                                some = true;
+                            }
+                            part = part || lo > 0 || hi < kTile;
+                            if (biased) bias = make_float2(a.mods.slopes[kvh * G + head_of[k]] * kLog2e, (float)(a.mods.pos0 + tok - key0));
+                        }
+                        mine->seen[lane + 32 * k] = sees;
+                        mine->bias[lane + 32 * k] = bias;
+                    }
+                    some = __any_sync(0xffffffffu, some);
+                    part = __any_sync(0xffffffffu, part);
+                    __syncwarp();
+                }
                 ok = mbar_wait(bar(M_DFULL + jc % kAccs), (jc / kAccs) & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t t_job = t_acc + (uint32_t)(jc % kAccs) * 128u;
-#pragma unroll 1
-                for (int c0 = 0; some && c0 < ncols; c0 += 16) {
-                    uint32_t v[16];
-                    KVF_TMEM_LD16(v, 0, t_job + c0);
-                    tmem_wait_ld();
-                    float2 x[8];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) x[c] = make_float2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                // C columns from c0 on, their dot products in v
+                auto add = [&](auto v, int c0, auto ncol) {
+                    constexpr int C = decltype(ncol)::value;
+                    auto dot = [&](int c) { return make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])); };
+                    int tier = 0;                // 0: no cap; 1, 2, 3: by the largest of my warp's scores (scores.cuh)
                     if (cap) {
+                        float far = 0.f;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) x[c] = make_float2(cap_any(a.mods, x[c].x), cap_any(a.mods, x[c].y));
+                        for (int c = 0; c < C; ++c) far = fmaxf(far, fabsf(__uint_as_float(v[c])));
+                        tier = !__any_sync(0xffffffffu, far > a.mods.small_to) ? 1 : !__any_sync(0xffffffffu, far > a.mods.middle_to) ? 2 : 3;
                     }
+                    if (tier == 2) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        Col p, q2;
-                        const uint32_t at = cols + (uint32_t)(c0 + 2 * c) * (uint32_t)sizeof(Col);
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=f"(p.neg), "=r"(p.seen), "=f"(p.slope), "=f"(p.at) : "r"(at));
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=f"(q2.neg), "=r"(q2.seen), "=f"(q2.slope), "=f"(q2.at) : "r"(at + 16u));
-                        float2 y = cap ? __fadd2_rn(x[c], make_float2(p.neg, q2.neg)) : __ffma2_rn(x[c], sl2, make_float2(p.neg, q2.neg));
-                        if (biased) {
-                            y.x = fmaf(-p.slope, fabsf(p.at - (float)r), y.x);
-                            y.y = fmaf(-q2.slope, fabsf(q2.at - (float)r), y.y);
+                        for (int c = 0; c < C; c += 2) {
+                            const float2 y = cap_middle(a.mods, dot(c));
+                            v[c] = __float_as_uint(y.x);
+                            v[c + 1] = __float_as_uint(y.y);
                         }
-                        if (part) {
-                            y.x = r >= (int)(p.seen & 0xFFFFu) && r < (int)(p.seen >> 16) ? y.x : -INFINITY;
-                            y.y = r >= (int)(q2.seen & 0xFFFFu) && r < (int)(q2.seen >> 16) ? y.y : -INFINITY;
+                    } else if (tier == 3) {
+#pragma unroll
+                        for (int c = 0; c < C; ++c) v[c] = __float_as_uint(cap_any(a.mods, __uint_as_float(v[c])));
+                    }
+                    auto sum_up = [&](auto exponent) {
+#pragma unroll
+                        for (int c = 0; c < C; c += 4) {
+                            float4 n4;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(n4.x), "=f"(n4.y), "=f"(n4.z), "=f"(n4.w) : "r"(neg + (uint32_t)(c0 + c) * 4u));
+                            const float2 y0 = exponent(c, make_float2(n4.x, n4.y)), y1 = exponent(c + 2, make_float2(n4.z, n4.w));
+                            acc0 = __fadd2_rn(acc0, make_float2(ex2(y0.x), ex2(y0.y)));
+                            acc1 = __fadd2_rn(acc1, make_float2(ex2(y1.x), ex2(y1.y)));
                         }
-                        const float2 e = make_float2(ex2(y.x), ex2(y.y));
-                        if (c & 1) acc1 = __fadd2_rn(acc1, e);
-                        else acc0 = __fadd2_rn(acc0, e);
+                    };
+                    if (part || biased) {
+                        const float2 by = cap ? both(1.f) : sl2;
+                        sum_up([&](int c, float2 n2) {
+                            float2 y = tier == 1 ? __ffma2_rn(dot(c), cap_small_over(a.mods, dot(c)), n2) : __ffma2_rn(dot(c), by, n2);
+                            const float2 b0 = mine->bias[c0 + c], b1 = mine->bias[c0 + c + 1];
+                            const uint32_t s0 = mine->seen[c0 + c], s1 = mine->seen[c0 + c + 1];
+                            if (biased) {
+                                y.x = fmaf(-b0.x, fabsf(b0.y - (float)r), y.x);
+                                y.y = fmaf(-b1.x, fabsf(b1.y - (float)r), y.y);
+                            }
+                            if (part) {
+                                y.x = r >= (int)(s0 & 0xFFFFu) && r < (int)(s0 >> 16) ? y.x : -INFINITY;
+                                y.y = r >= (int)(s1 & 0xFFFFu) && r < (int)(s1 >> 16) ? y.y : -INFINITY;
+                            }
+                            return y;
+                        });
+                    } else if (tier == 0) {
+                        sum_up([&](int c, float2 n2) { return __ffma2_rn(dot(c), sl2, n2); });
+                    } else if (tier == 1) {
+                        sum_up([&](int c, float2 n2) { return __ffma2_rn(dot(c), cap_small_over(a.mods, dot(c)), n2); });
+                    } else {
+                        sum_up([&](int c, float2 n2) { return __fadd2_rn(dot(c), n2); });
+                    }
+                };
+                if (kOne) {
+#pragma unroll 1
+                    for (int c0 = 0; some && c0 < ncols; c0 += 16) {
+                        uint32_t v[16];
+                        __syncwarp();
+                        KVF_TMEM_LD16(v, 0, t_job + c0);
+                        tmem_wait_ld();
+                        add(v, c0, std::integral_constant<int, 16>{});
+                    }
+                } else if (some) {
+                    // 32 columns at a time, the next ones on their way
+                    uint32_t v[2][32];
+                    __syncwarp();
+                    KVF_TMEM_LD32(v[0], 0, t_job);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        __syncwarp();
+                        tmem_wait_ld();
+                        if (h < 3) KVF_TMEM_LD32(v[(h + 1) & 1], 0, t_job + 32 * (h + 1));
+                        add(v[h & 1], 32 * h, std::integral_constant<int, 32>{});
                     }
                 }
                 tc_fence_before();

@@ -212,3 +212,111 @@ def test_a_bounded_fold():
             assert torch.equal(kept.cpu(), scored.kept_rows(mass, len(here), 4, n, budget))
             caches, mass, spare = caches[::-1], spare, mass
     assert all(c.status() == binding.KVF_OK for c in caches)
+
+
+def paged_pair(rows, n, seed=0, h=8, kv=2):
+    """A contiguous and a paged cache (pages in no order) that hold the same rows."""
+    cfg = binding.make_config(h, kv, 128, "bf16", rows + n, max(n, 1), rope_base=BASE)
+    pages = (rows + n + 127) // 128
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    pool = torch.zeros(binding.paged_pool_bytes(cfg, pages + 3), dtype=torch.uint8, device="cuda")
+    table = torch.randperm(pages + 3, generator=gen, device="cuda")[:pages].to(torch.int32)
+    flat, paged = binding.Cache(cfg), binding.PagedCache(cfg, pool, pages + 3, table)
+    flat.storage.zero_()
+    for kvi, plane in enumerate((flat.k_plane(), flat.v_plane())):
+        plane[:, :rows] = torch.randn((kv, rows, 128), generator=gen, device="cuda")
+        padded = torch.zeros((kv, pages * 128, 128), dtype=torch.bfloat16, device="cuda")
+        padded[:, :rows] = plane[:, :rows]
+        paged.page_rows(kvi)[table.long()] = padded.view(kv, pages, 128, 128).transpose(0, 1)
+    flat.set_len(rows)
+    paged.set_len(rows)
+    return flat, paged, gen
+
+
+@pytest.mark.parametrize("n", [1, 40, 200])
+def test_paged_caches_give_the_bits_of_contiguous_ones(n):
+    rows = 1500
+    flat, paged, gen = paged_pair(rows, n)
+    q, k, v = chunk(flat, gen, n)
+    kw = dict(softcap=12.0, first=torch.randint(0, rows, (n,), generator=gen, device="cuda", dtype=torch.int32), slopes=slopes_of(8))
+    got = []
+    for cache in (flat, paged):
+        lse = torch.empty((n, 8), device="cuda")
+        out = cache.fold_step(q, k, v, lse=lse, **kw)
+        got.append((out, lse, cache.mass(cache.rotate(q), lse, **kw)))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("heads,dtype", [((32, 8, 128), "bf16"), ((28, 4, 128), "bf16"), ((8, 2, 128), "f32")])
+@pytest.mark.parametrize("n", [1, 300])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_mass_of_rows_that_nobody_sees_is_nothing_whatever_they_hold(heads, dtype, n, bad):
+    rows = 700
+    cache, gen = make(heads, dtype, 800, 300, prefix=rows, seed=4)
+    q = chunk(cache, gen, n)[0]
+    lse = torch.randn((n, heads[0]), generator=gen, device="cuda") + 7
+    first = torch.full((n,), 290, dtype=torch.int32, device="cuda")
+    clean = cache.mass(q, lse, first=first)
+    cache.k_plane()[:, 100:290] = bad
+    dirty = cache.mass(q, lse, first=first)
+    assert torch.equal(clean, dirty) and bool((clean[:, :290] == 0).all())
+
+
+def test_operators_side_by_side_on_two_streams():
+    """Two caches with workspaces of their own, a bounded fold on each, at the same time and one after the other: the same bits."""
+    def run(stream, seed):
+        a, gen = make((8, 2, 128), "bf16", 1300, 200, prefix=1000, seed=seed)
+        b, _ = make((8, 2, 128), "bf16", 1300, 200)
+        stream.wait_stream(torch.cuda.current_stream())
+        got = []
+        with torch.cuda.stream(stream):
+            mass = torch.rand((2, 1300), generator=gen, device="cuda")
+            for _ in range(4):
+                q, k, v = chunk(a, gen, 150)
+                lse = torch.empty((150, 8), device="cuda")
+                got.append(a.fold_step(q, k, v, lse=lse, softcap=9.0))
+                a.mass(a.rotate(q), lse, mass=mass, out=mass, softcap=9.0)
+                left = torch.zeros_like(mass)
+                got.append(a.evict(b, mass, 1000, n_sink=2, n_recent=100, mass_out=left))
+                a, b, mass = b, a, left
+            got.append(mass)
+        return got
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    both = run(one, 1), run(two, 2)
+    torch.cuda.synchronize()
+    alone = []
+    for seed in (1, 2):
+        alone.append(run(torch.cuda.current_stream(), seed))
+        torch.cuda.synchronize()
+    for x, y in zip(both, alone):
+        assert all(torch.equal(p, q) for p, q in zip(x, y))
+
+
+def test_captured_mass_and_eviction_replay_on_new_weights():
+    src, gen = make((8, 2, 128), "bf16", 900, 64, prefix=900, seed=3)
+    dst, _ = make((8, 2, 128), "bf16", 500, 1)
+    q = chunk(src, gen, 64)[0]
+    lse = torch.randn((64, 8), generator=gen, device="cuda") + 7
+    mass, out, left = torch.zeros((2, 900), device="cuda"), torch.zeros((2, 900), device="cuda"), torch.zeros((2, 500), device="cuda")
+    kept = torch.zeros((2, 500), dtype=torch.int32, device="cuda")
+
+    def steps():
+        src.mass(q, lse, mass=mass, out=out)
+        src.evict(dst, out, 500, n_sink=4, n_recent=64, mass_out=left, kept=kept)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        steps()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            steps()
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        mass.copy_(torch.rand(mass.shape, generator=gen, device="cuda"))
+        q.copy_(chunk(src, gen, 64)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, src.mass(q, lse, mass=mass))
+        assert torch.equal(kept.cpu(), scored.kept_rows(out, 900, 4, 64, 500))
+        same_rows(src, dst, kept)
