@@ -8,7 +8,7 @@
 // query heads), so that a thread has one key's row of tensor memory and the sum over queries is its own: what would be a reduction
 // over lanes in the attention kernels costs nothing here.  Per (KV head, key tile) the K tile stays in shared memory while the query
 // tiles come by (L2 holds them); where the chunk is one query tile that one stays and the keys stream.  Jobs (one query tile
-// against one key tile) go to two groups of four warps in turn, four accumulators of 128 columns deep.
+// against one key tile) go to four groups of four warps in turn, each with an accumulator of 128 columns.
 // What bounds it: one exponential per score, 1024 cycles of the special-function unit for a tile whose MMAs take 512; a decoded token is
 // bound by the K plane's bytes.
 #include <type_traits>
@@ -23,14 +23,16 @@ namespace {
 // ---- tensor cores
 constexpr int kTile = 128, kD = 128;
 constexpr uint32_t kPanel = 128 * 128, kTileBytes = 2 * kPanel;
-constexpr int kTcThreads = 384;                // warp 0 TMA, warp 1 MMA (2 and 3 idle), warps 4 - 11 exponentials
+constexpr int kGroups = 4;                     // groups of four warps that take the jobs in turn
+constexpr int kTcThreads = 128 + kGroups * 128;        // warp 0 TMA, warp 1 MMA (2 and 3 idle), the others exponentials
 constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: two K slots, four Q slots; one: five and one
-constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory
+constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory: one a group
 constexpr uint32_t kTmemCols = 512;
 struct __align__(16) Cols {                    // what a warp knows of a job's columns (query rows)
     float neg[kTile];                          // -lse * log2(e) (-inf: no such row, or it saw nothing)
-    uint32_t seen[kTile];                      // keys of the tile that it sees, [low half, high half); filled where some may not be
     float2 bias[kTile];                        // slope in log2 units, distance of the tile's first key; filled under slopes
+    uint16_t seen[kTile];                      // keys of the tile that it sees, [low byte, high byte); filled where some may not be
+    float sum[32];                             // the warp's sums on their way to the first group
 };
 enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + kAccs,
        M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_COUNT };
@@ -38,10 +40,9 @@ struct MassCtl {
     unsigned long long bars[M_COUNT];
     uint32_t tmem_base;
     int abort;
-    float sums[kTile];                         // the second group's sums on their way to the first
 };
-constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // for each of the eight warps
-constexpr uint32_t kOffMassCtl = kOffCols + 8 * sizeof(Cols);
+constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // for each warp of exponentials
+constexpr uint32_t kOffMassCtl = kOffCols + kGroups * 4 * sizeof(Cols);
 constexpr uint32_t kMassSmem = kOffMassCtl + 1024 + 1024;
 static_assert(sizeof(MassCtl) <= 1024 && kMassSmem <= 232448, "shared memory budget of one CTA");
 
@@ -88,7 +89,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         for (int s = 0; s < SK; ++s) { mbar_init(bar(M_KFULL + s), 1); mbar_init(bar(M_KEMPTY + s), 1); }
         for (int s = 0; s < SQ; ++s) { mbar_init(bar(M_QFULL + s), 1); mbar_init(bar(M_QEMPTY + s), 1); }
         for (int s = 0; s < kAccs; ++s) { mbar_init(bar(M_DFULL + s), 1); mbar_init(bar(M_DEMPTY + s), 4); }
-        for (int s = 0; s < 4; ++s) { mbar_init(bar(M_SUM + s), 1); mbar_init(bar(M_TAKEN + s), 1); }
+        for (int s = 0; s < 4; ++s) { mbar_init(bar(M_SUM + s), kGroups - 1); mbar_init(bar(M_TAKEN + s), 1); }
         mbar_init(bar(M_DRAIN), 1);
         ctl->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -238,7 +239,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                     if (ai < i1) w.item(a, ai, akvh, akt, asplit, aq, aq1);
                 }
                 ++aj;
-            } while (ai < i1 && (aj & 1) != group);
+            } while (ai < i1 && aj % kGroups != group);
             if (ai < i1) load_neg(akvh, aq, ahead);
         };
         if (!kOne) look_ahead();
@@ -251,7 +252,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             float2 acc0 = both(0.f), acc1 = both(0.f);
             const int jc0 = jc;
             for (int q = q0; q < q1; ++q, ++jc) {
-                if ((jc & 1) != group) continue;
+                if (jc % kGroups != group) continue;
                 if (!kOne) {
                     put_neg(ahead);
                     look_ahead();
@@ -274,13 +275,13 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                             const RowRange seen = a.scored ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, P + (int64_t)(tok + 1) * a.self_rows};
                             const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kTile), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kTile);
                             if (lo < hi) {
-                                sees = (uint32_t)lo | (uint32_t)hi << 16;
+                                sees = (uint32_t)lo | (uint32_t)hi << 8;
                                 some = true;
                             }
                             part = part || lo > 0 || hi < kTile;
                             if (biased) bias = make_float2(a.mods.slopes[kvh * G + head_of[k]] * kLog2e, (float)(a.mods.pos0 + tok - key0));
                         }
-                        mine->seen[lane + 32 * k] = sees;
+                        mine->seen[lane + 32 * k] = (uint16_t)sees;
                         mine->bias[lane + 32 * k] = bias;
                     }
                     some = __any_sync(0xffffffffu, some);
@@ -335,8 +336,8 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                                 y.y = fmaf(-b1.x, fabsf(b1.y - (float)r), y.y);
                             }
                             if (part) {
-                                y.x = r >= (int)(s0 & 0xFFFFu) && r < (int)(s0 >> 16) ? y.x : -INFINITY;
-                                y.y = r >= (int)(s1 & 0xFFFFu) && r < (int)(s1 >> 16) ? y.y : -INFINITY;
+                                y.x = r >= (int)(s0 & 0xFFu) && r < (int)(s0 >> 8) ? y.x : -INFINITY;
+                                y.y = r >= (int)(s1 & 0xFFu) && r < (int)(s1 >> 8) ? y.y : -INFINITY;
                             }
                             return y;
                         });
@@ -348,26 +349,16 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         sum_up([&](int c, float2 n2) { return __fadd2_rn(dot(c), n2); });
                     }
                 };
-                if (kOne) {
+                if (some) {
+                    constexpr int C = kOne ? 16 : 32;
 #pragma unroll 1
-                    for (int c0 = 0; some && c0 < ncols; c0 += 16) {
-                        uint32_t v[16];
+                    for (int c0 = 0; c0 < (kOne ? ncols : kTile); c0 += C) {
+                        uint32_t v[C];
                         __syncwarp();
-                        KVF_TMEM_LD16(v, 0, t_job + c0);
+                        if constexpr (kOne) KVF_TMEM_LD16(v, 0, t_job + c0);
+                        else KVF_TMEM_LD32(v, 0, t_job + c0);
                         tmem_wait_ld();
-                        add(v, c0, std::integral_constant<int, 16>{});
-                    }
-                } else if (some) {
-                    // 32 columns at a time, the next ones on their way
-                    uint32_t v[2][32];
-                    __syncwarp();
-                    KVF_TMEM_LD32(v[0], 0, t_job);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        __syncwarp();
-                        tmem_wait_ld();
-                        if (h < 3) KVF_TMEM_LD32(v[(h + 1) & 1], 0, t_job + 32 * (h + 1));
-                        add(v[h & 1], 32 * h, std::integral_constant<int, 32>{});
+                        add(v, c0, std::integral_constant<int, C>{});
                     }
                 }
                 tc_fence_before();
@@ -378,15 +369,15 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             const float2 acc = __fadd2_rn(acc0, acc1);
             float sum = acc.x + acc.y;
             if (kOne) {
-                if (jc == jc0 ? group != 0 : (jc0 & 1) != group) continue;           // the other group had the job
+                if (jc == jc0 ? group != 0 : jc0 % kGroups != group) continue;           // the other group had the job
             } else {
-                // the second group's sum of the key goes to the first
+                // the other groups' sums of the key go to the first
                 ++sums;
-                if (group == 1) {
+                if (group > 0) {
                     if (sums > 1) ok = mbar_wait(bar(M_TAKEN + quarter), (sums - 2) & 1, ctl, a.status);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    *reinterpret_cast<volatile float *>(&ctl->sums[r]) = sum;
+                    *reinterpret_cast<volatile float *>(&mine->sum[lane]) = sum;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(M_SUM + quarter));
                     continue;
@@ -394,7 +385,8 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 ok = mbar_wait(bar(M_SUM + quarter), (sums - 1) & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                sum += *reinterpret_cast<volatile float *>(&ctl->sums[r]);
+#pragma unroll
+                for (int o = 1; o < kGroups; ++o) sum += *reinterpret_cast<volatile float *>(&mine[4 * o].sum[lane]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(M_TAKEN + quarter));
             }
