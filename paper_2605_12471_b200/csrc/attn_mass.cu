@@ -11,6 +11,7 @@
 // against one key tile) go to four groups of four warps in turn, each with an accumulator of 128 columns.
 // What bounds it: one exponential per score, 1024 cycles of the special-function unit for a tile whose MMAs take 512; a decoded token is
 // bound by the K plane's bytes.
+#include <cstddef>
 #include <type_traits>
 
 #include "kvfold_internal.h"
@@ -24,27 +25,31 @@ namespace {
 constexpr int kTile = 128, kD = 128;
 constexpr uint32_t kPanel = 128 * 128, kTileBytes = 2 * kPanel;
 constexpr int kGroups = 4;                     // groups of four warps that take the jobs in turn
-constexpr int kTcThreads = 128 + kGroups * 128;        // warp 0 TMA, warp 1 MMA (2 and 3 idle), the others exponentials
+constexpr int kTcThreads = 128 + kGroups * 128;        // warp 0 TMA, warp 1 MMA, warps 2 and 3 what is to be known of the columns, the others exponentials
 constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: two K slots, four Q slots; one: five and one
 constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory: one a group
 constexpr uint32_t kTmemCols = 512;
-struct __align__(16) Cols {                    // what a warp knows of a job's columns (query rows)
+constexpr int kColSlots = 8;
+struct __align__(16) Cols {                    // what the exponentials need to know of a job's columns (query rows)
     float neg[kTile];                          // -lse * log2(e) (-inf: no such row, or it saw nothing)
     float2 bias[kTile];                        // slope in log2 units, distance of the tile's first key; filled under slopes
     uint16_t seen[kTile];                      // keys of the tile that it sees, [low byte, high byte); filled where some may not be
-    float sum[32];                             // the warp's sums on their way to the first group
+    int some, part;                            // does any column see a key of the tile; may one not see all of them
+    int pad[2];
 };
 enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + kAccs,
-       M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_COUNT };
+       M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_CFULL, M_CEMPTY = M_CFULL + kColSlots,
+       M_COUNT = M_CEMPTY + kColSlots };
 struct MassCtl {
     unsigned long long bars[M_COUNT];
     uint32_t tmem_base;
     int abort;
+    float sums[kGroups - 1][kTile];            // the other groups' sums on their way to the first
 };
-constexpr uint32_t kOffCols = kSlots * kTileBytes;                          // for each warp of exponentials
-constexpr uint32_t kOffMassCtl = kOffCols + kGroups * 4 * sizeof(Cols);
-constexpr uint32_t kMassSmem = kOffMassCtl + 1024 + 1024;
-static_assert(sizeof(MassCtl) <= 1024 && kMassSmem <= 232448, "shared memory budget of one CTA");
+constexpr uint32_t kOffCols = kSlots * kTileBytes;
+constexpr uint32_t kOffMassCtl = kOffCols + kColSlots * sizeof(Cols);
+constexpr uint32_t kMassSmem = kOffMassCtl + 2560 + 1024;
+static_assert(sizeof(MassCtl) <= 2560 && kMassSmem <= 232448, "shared memory budget of one CTA");
 
 __device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
@@ -90,6 +95,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         for (int s = 0; s < SQ; ++s) { mbar_init(bar(M_QFULL + s), 1); mbar_init(bar(M_QEMPTY + s), 1); }
         for (int s = 0; s < kAccs; ++s) { mbar_init(bar(M_DFULL + s), 1); mbar_init(bar(M_DEMPTY + s), 4); }
         for (int s = 0; s < 4; ++s) { mbar_init(bar(M_SUM + s), kGroups - 1); mbar_init(bar(M_TAKEN + s), 1); }
+        for (int s = 0; s < kColSlots; ++s) { mbar_init(bar(M_CFULL + s), 1); mbar_init(bar(M_CEMPTY + s), 4); }
         mbar_init(bar(M_DRAIN), 1);
         ctl->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -197,15 +203,9 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             tc_commit(bar(M_DRAIN));
             mbar_wait_drain(bar(M_DRAIN), 0, a.status);
         }
-    } else if (warp >= 4) {
-        // ------------------------------------------------------------------ exponentials: a thread per key
-        const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-        const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16);
-        Cols *mine = reinterpret_cast<Cols *>(smem + kOffCols) + (warp - 4);
-        const uint32_t neg = smem_u32(mine->neg);
-        const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
-        const bool ranged = a.scored && (a.mods.first || a.mods.end);
-        const float2 sl2 = both(a.scale_log2);
+    } else if (warp < 4) {
+        // ------------------------------------------------------------------ columns of the jobs, up to eight jobs ahead, two warps in turn
+        const bool biased = a.scored && a.mods.slopes, ranged = a.scored && (a.mods.first || a.mods.end);
         // my four columns of a query tile: 32 apart, token and head within the group
         int tok_of[4], head_of[4];
 #pragma unroll
@@ -213,59 +213,30 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             tok_of[k] = (lane + 32 * k) / G;
             head_of[k] = (lane + 32 * k) % G;
         }
-        // denominators of a query tile, as they enter an exponent
-        auto load_neg = [&](int kvh, int q, float (&l)[4]) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int tok = q * w.toks + tok_of[k];
-                l[k] = tok_of[k] < w.toks && tok < a.n ? a.lse[(int64_t)tok * a.H + kvh * G + head_of[k]] : -INFINITY;
-            }
-        };
-        auto put_neg = [&](const float (&l)[4]) {
-            __syncwarp();                        // (the last ones are read)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mine->neg[lane + 32 * k] = l[k] == -INFINITY ? -INFINITY : -l[k] * kLog2e;
-            __syncwarp();
-        };
-        // My jobs' query tiles one ahead: the denominators come from memory while the job before is worked on.
-        float ahead[4];
-        int64_t ai = i0 - istep;
-        int aq = 0, aq1 = 0, aj = -1, akvh = 0, akt, asplit;
-        auto look_ahead = [&]() {
-            do {
-                ++aq;
-                while (aq >= aq1 && ai < i1) {
-                    ai += istep;
-                    if (ai < i1) w.item(a, ai, akvh, akt, asplit, aq, aq1);
-                }
-                ++aj;
-            } while (ai < i1 && aj % kGroups != group);
-            if (ai < i1) load_neg(akvh, aq, ahead);
-        };
-        if (!kOne) look_ahead();
-        int jc = 0, sums = 0, held = -1;
+        int jc = 0;
         bool ok = true;
         for (int64_t i = i0; ok && i < i1; i += istep) {
             int kvh, kt, split, q0, q1;
             w.item(a, i, kvh, kt, split, q0, q1);
             const int64_t key0 = (int64_t)kt * kTile;
-            float2 acc0 = both(0.f), acc1 = both(0.f);
-            const int jc0 = jc;
             for (int q = q0; q < q1; ++q, ++jc) {
-                if (jc % kGroups != group) continue;
-                if (!kOne) {
-                    put_neg(ahead);
-                    look_ahead();
-                } else if (held != kvh) {
-                    load_neg(kvh, q, ahead);
-                    put_neg(ahead);
-                    held = kvh;
+                if ((jc & 1) != warp - 2) continue;
+                float l[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int tok = q * w.toks + tok_of[k];
+                    l[k] = tok_of[k] < w.toks && tok < a.n ? a.lse[(int64_t)tok * a.H + kvh * G + head_of[k]] : -INFINITY;
                 }
+                Cols *cols = reinterpret_cast<Cols *>(smem + kOffCols) + jc % kColSlots;
+                ok = mbar_wait(bar(M_CEMPTY + jc % kColSlots), ((jc / kColSlots) & 1) ^ 1, ctl, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) cols->neg[lane + 32 * k] = l[k] == -INFINITY ? -INFINITY : -l[k] * kLog2e;
                 // does every token see all of the key tile?  (without ranges known from the tile's first token)
                 bool some = true, part = ranged || key0 + kTile > P + (int64_t)(q * w.toks + 1) * a.self_rows;
                 if (part || biased) {
                     some = part = false;
-                    __syncwarp();
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int tok = q * w.toks + tok_of[k];
@@ -281,13 +252,42 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                             part = part || lo > 0 || hi < kTile;
                             if (biased) bias = make_float2(a.mods.slopes[kvh * G + head_of[k]] * kLog2e, (float)(a.mods.pos0 + tok - key0));
                         }
-                        mine->seen[lane + 32 * k] = (uint16_t)sees;
-                        mine->bias[lane + 32 * k] = bias;
+                        cols->seen[lane + 32 * k] = (uint16_t)sees;
+                        cols->bias[lane + 32 * k] = bias;
                     }
                     some = __any_sync(0xffffffffu, some);
                     part = __any_sync(0xffffffffu, part);
-                    __syncwarp();
                 }
+                if (lane == 0) {
+                    cols->some = some;
+                    cols->part = part;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(M_CFULL + jc % kColSlots));
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ exponentials: a thread per key
+        const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16);
+        const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
+        const float2 sl2 = both(a.scale_log2);
+        int jc = 0, sums = 0;
+        bool ok = true;
+        for (int64_t i = i0; ok && i < i1; i += istep) {
+            int kvh, kt, split, q0, q1;
+            w.item(a, i, kvh, kt, split, q0, q1);
+            const int64_t key0 = (int64_t)kt * kTile;
+            float2 acc0 = both(0.f), acc1 = both(0.f);
+            const int jc0 = jc;
+            for (int q = q0; q < q1; ++q, ++jc) {
+                if (jc % kGroups != group) continue;
+                const Cols *cols = reinterpret_cast<const Cols *>(smem + kOffCols) + jc % kColSlots;
+                const uint32_t neg = base + kOffCols + (uint32_t)(jc % kColSlots) * (uint32_t)sizeof(Cols);
+                ok = mbar_wait(bar(M_CFULL + jc % kColSlots), (jc / kColSlots) & 1, ctl, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const bool some = *reinterpret_cast<const volatile int *>(&cols->some), part = *reinterpret_cast<const volatile int *>(&cols->part);
                 ok = mbar_wait(bar(M_DFULL + jc % kAccs), (jc / kAccs) & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -329,13 +329,17 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         const float2 by = cap ? both(1.f) : sl2;
                         sum_up([&](int c, float2 n2) {
                             float2 y = tier == 1 ? __ffma2_rn(dot(c), cap_small_over(a.mods, dot(c)), n2) : __ffma2_rn(dot(c), by, n2);
-                            const float2 b0 = mine->bias[c0 + c], b1 = mine->bias[c0 + c + 1];
-                            const uint32_t s0 = mine->seen[c0 + c], s1 = mine->seen[c0 + c + 1];
                             if (biased) {
+                                float2 b0, b1;
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b0.x), "=f"(b0.y), "=f"(b1.x), "=f"(b1.y)
+                                             : "r"(neg + (uint32_t)offsetof(Cols, bias) + (uint32_t)(c0 + c) * 8u));
                                 y.x = fmaf(-b0.x, fabsf(b0.y - (float)r), y.x);
                                 y.y = fmaf(-b1.x, fabsf(b1.y - (float)r), y.y);
                             }
                             if (part) {
+                                uint32_t s01;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s01) : "r"(neg + (uint32_t)offsetof(Cols, seen) + (uint32_t)(c0 + c) * 2u));
+                                const uint32_t s0 = s01 & 0xFFFFu, s1 = s01 >> 16;
                                 y.x = r >= (int)(s0 & 0xFFu) && r < (int)(s0 >> 8) ? y.x : -INFINITY;
                                 y.y = r >= (int)(s1 & 0xFFu) && r < (int)(s1 >> 8) ? y.y : -INFINITY;
                             }
@@ -363,7 +367,10 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(M_DEMPTY + jc % kAccs));
+                if (lane == 0) {
+                    mbar_arrive(bar(M_DEMPTY + jc % kAccs));
+                    mbar_arrive(bar(M_CEMPTY + jc % kColSlots));
+                }
             }
             if (!ok) break;
             const float2 acc = __fadd2_rn(acc0, acc1);
@@ -377,7 +384,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                     if (sums > 1) ok = mbar_wait(bar(M_TAKEN + quarter), (sums - 2) & 1, ctl, a.status);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    *reinterpret_cast<volatile float *>(&mine->sum[lane]) = sum;
+                    *reinterpret_cast<volatile float *>(&ctl->sums[group - 1][r]) = sum;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(M_SUM + quarter));
                     continue;
@@ -386,7 +393,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
 #pragma unroll
-                for (int o = 1; o < kGroups; ++o) sum += *reinterpret_cast<volatile float *>(&mine[4 * o].sum[lane]);
+                for (int o = 1; o < kGroups; ++o) sum += *reinterpret_cast<volatile float *>(&ctl->sums[o - 1][r]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(M_TAKEN + quarter));
             }
