@@ -6,11 +6,11 @@
 //
 // bf16 rows run on the tensor cores.  A tile is S^T = K Q^T, 128 keys of one KV head by up to 128 query rows (whole tokens of its G
 // query heads), so that a thread has one key's row of tensor memory and the sum over queries is its own: what would be a reduction
-// over lanes in the attention kernels costs nothing here.  Per (KV head, key tile) the K tile stays in shared memory while the query
-// tiles come by (L2 holds them); where the chunk is one query tile that one stays and the keys stream.  Jobs (one query tile
-// against one key tile) go to four groups of four warps in turn, each with an accumulator of 128 columns.
-// What bounds it: one exponential per score, 1024 cycles of the special-function unit for a tile whose MMAs take 512; a decoded token is
-// bound by the K plane's bytes.
+// over lanes in the attention kernels costs nothing here.  An item is two key tiles, which stay in shared memory while the query
+// tiles come by (L2 holds them); where the chunk is one query tile that one stays and the keys stream.
+// What bounds it: shared memory (per tile of 128 x 128: the MMAs' operands 512 cycles, half a query tile coming in 128, the columns'
+// denominators 64) beside one exponential per score, 1024 cycles of the special-function unit, of which a quarter goes through the
+// multiply-add pipe.  A decoded token is bound by the K plane's bytes.
 #include <cstddef>
 #include <type_traits>
 
@@ -22,50 +22,68 @@ namespace kvf {
 namespace {
 
 // ---- tensor cores
-constexpr int kTile = 128, kD = 128;
+constexpr int kTile = 128, kD = 128, kUnit = 2 * kTile;      // keys of a tile, of an item
 constexpr uint32_t kPanel = 128 * 128, kTileBytes = 2 * kPanel;
-constexpr int kGroups = 4;                     // groups of four warps that take the jobs in turn
+constexpr int kGroups = 4;                     // groups of four warps of exponentials (a warp has a quarter of the lanes)
 constexpr int kTcThreads = 128 + kGroups * 128;        // warp 0 TMA, warp 1 MMA, warps 2 and 3 what is to be known of the columns, the others exponentials
-constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: two K slots, four Q slots; one: five and one
-constexpr int kAccs = 4;                       // accumulators of 128 columns in tensor memory: one a group
-constexpr uint32_t kTmemCols = 512;
+constexpr int kSlots = 6;                      // tiles in shared memory: many query tiles: four K slots, two Q slots; one: five and one
+constexpr uint32_t kTmemCols = 512;            // two sets of two accumulators of 128 columns
 constexpr int kColSlots = 8;
 struct __align__(16) Cols {                    // what the exponentials need to know of a job's columns (query rows)
     float neg[kTile];                          // -lse * log2(e) (-inf: no such row, or it saw nothing)
-    float2 bias[kTile];                        // slope in log2 units, distance of the tile's first key; filled under slopes
-    uint16_t seen[kTile];                      // keys of the tile that it sees, [low byte, high byte); filled where some may not be
-    int some, part;                            // does any column see a key of the tile; may one not see all of them
+    float2 bias[kTile];                        // slope in log2 units, distance of the item's first key; filled under slopes
+    uint32_t seen[kTile];                      // keys of the item that it sees, [low half, high half); filled where some may not be
+    int some, part;                            // does any column see a key of the item; may one not see all of them
     int pad[2];
 };
-enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + kAccs,
-       M_SUM = M_DEMPTY + kAccs, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_CFULL, M_CEMPTY = M_CFULL + kColSlots,
-       M_COUNT = M_CEMPTY + kColSlots };
+enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 2, M_DFULL = M_QEMPTY + 2, M_DEMPTY = M_DFULL + 2,
+       M_SUM = M_DEMPTY + 2, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_CFULL, M_CEMPTY = M_CFULL + kColSlots, M_COUNT = M_CEMPTY + kColSlots };
 struct MassCtl {
     unsigned long long bars[M_COUNT];
     uint32_t tmem_base;
     int abort;
-    float sums[kGroups - 1][kTile];            // the other groups' sums on their way to the first
+    float sums[kGroups - 1][kUnit];            // the other groups' sums on their way to the first
 };
 constexpr uint32_t kOffCols = kSlots * kTileBytes;
-constexpr uint32_t kOffMassCtl = kOffCols + kColSlots * sizeof(Cols);
-constexpr uint32_t kMassSmem = kOffMassCtl + 2560 + 1024;
-static_assert(sizeof(MassCtl) <= 2560 && kMassSmem <= 232448, "shared memory budget of one CTA");
+constexpr uint32_t kOffMassCtl = kOffCols + (kColSlots * sizeof(Cols) + 1023) / 1024 * 1024;
+constexpr uint32_t kMassSmem = kOffMassCtl + 4096 + 1024;
+static_assert(sizeof(MassCtl) <= 4096 && kMassSmem <= 232448, "shared memory budget of one CTA");
 
 __device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
+__device__ __forceinline__ void lds128(uint32_t at, float (&x)[4]) {
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(at));
+}
 
-// What the roles have to agree on.  Item = (KV head, key tile, split of the query tiles); its jobs are query tiles [q0, q1).
+// 2^x of a pair of numbers without the special-function unit: x = i + f, |f| <= 1/2, 2^f = 1 + f c1 + ... + f^5 c5 (least relative
+// error, 9e-8, by Lawson's reweighting; in fp32 1.6e-7, as good as ex2.approx), i added to the exponent.  Below 2^-126 off by less than
+// 2^-126, from 2^128 on infinite; NaN counts as -inf.
+__device__ __forceinline__ float2 exp2_fma(float2 x) {
+    x.x = fminf(fmaxf(x.x, -127.f), 128.f);
+    x.y = fminf(fmaxf(x.y, -127.f), 128.f);
+    const float2 magic = both(12582912.f);                         // 1.5 * 2^23: the sum's low bits are the nearest whole number
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 f = __fadd2_rn(x, __ffma2_rn(t, both(-1.f), magic));
+    float2 y = __ffma2_rn(f, both(0.0013264727123542784f), both(0.009671512644823185f));
+    y = __ffma2_rn(f, y, both(0.0555073374349718f));
+    y = __ffma2_rn(f, y, both(0.24022242085262321f));
+    y = __ffma2_rn(f, y, both(0.6931469775989922f));
+    y = __ffma2_rn(f, y, both(1.f));
+    return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(t.y) << 23)));
+}
+
+// What the roles have to agree on.  Item = (KV head, 256 keys, split of the query tiles); its jobs are query tiles [q0, q1).
 struct MassWork {
-    int nkt, nq, toks, splits, one;            // key tiles of a KV head, query tiles, tokens of a query tile
+    int nkt, nku, nq, toks, splits, one;       // key tiles and items' worth of keys of a KV head, query tiles, tokens of a query tile
     int64_t items;                             // (below 2^31)
-    __device__ __forceinline__ void item(const MassArgs &a, int64_t i, int &kvh, int &kt, int &split, int &q0, int &q1) const {
+    __device__ __forceinline__ void item(const MassArgs &a, int64_t i, int &kvh, int &ku, int &split, int &q0, int &q1) const {
         const uint32_t u = (uint32_t)i / (uint32_t)splits;
         split = (int)((uint32_t)i - u * (uint32_t)splits);
-        kvh = (int)(u / (uint32_t)nkt);
-        kt = (int)u - kvh * nkt;
-        // (without ranges, tokens whose row lies below the key tile see none of it)
-        const int64_t ahead = (int64_t)kt * kTile - (a.rows - a.n);
+        kvh = (int)(u / (uint32_t)nku);
+        ku = (int)u - kvh * nku;
+        // (without ranges, tokens whose row lies below the item's keys see none of them)
+        const int64_t ahead = (int64_t)ku * kUnit - (a.rows - a.n);
         int from = 0;
         if (a.self_rows && !(a.scored && (a.mods.first || a.mods.end)) && ahead > 0) from = (int)(ahead / toks);
         q0 = from + (int)((int64_t)split * (nq - from) / splits);
@@ -77,7 +95,10 @@ struct MassWork {
 template <bool kOne>
 __global__ void __launch_bounds__(kTcThreads, 1)
 mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
-    constexpr int SK = kOne ? 5 : 2, SQ = kOne ? 1 : 4;
+    constexpr int SK = kOne ? 5 : 4, SQ = kOne ? 1 : 2;
+    // Many query tiles: all groups share a job, each a quarter of its columns for both key tiles (a thread has two keys, and what it
+    // reads of a column serves both).  One: two groups, one for each key tile, take every other job.
+    constexpr int kTurns = kOne ? 2 : 1, kWarpsOfJob = 16 / kTurns;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - smem_u32(smem_raw));
@@ -93,9 +114,9 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
     if (threadIdx.x == 0) {
         for (int s = 0; s < SK; ++s) { mbar_init(bar(M_KFULL + s), 1); mbar_init(bar(M_KEMPTY + s), 1); }
         for (int s = 0; s < SQ; ++s) { mbar_init(bar(M_QFULL + s), 1); mbar_init(bar(M_QEMPTY + s), 1); }
-        for (int s = 0; s < kAccs; ++s) { mbar_init(bar(M_DFULL + s), 1); mbar_init(bar(M_DEMPTY + s), 4); }
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(M_DFULL + s), 1); mbar_init(bar(M_DEMPTY + s), kWarpsOfJob); }
         for (int s = 0; s < 4; ++s) { mbar_init(bar(M_SUM + s), kGroups - 1); mbar_init(bar(M_TAKEN + s), 1); }
-        for (int s = 0; s < kColSlots; ++s) { mbar_init(bar(M_CFULL + s), 1); mbar_init(bar(M_CEMPTY + s), 4); }
+        for (int s = 0; s < kColSlots; ++s) { mbar_init(bar(M_CFULL + s), 1); mbar_init(bar(M_CEMPTY + s), kWarpsOfJob); }
         mbar_init(bar(M_DRAIN), 1);
         ctl->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -127,22 +148,24 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             int kc = 0, qc = 0, held = -1;       // tiles loaded so far; kOne: KV head of the query tile held
             bool ok = true;
             for (int64_t i = i0; ok && i < i1; i += istep) {
-                int kvh, kt, split, q0, q1;
-                w.item(a, i, kvh, kt, split, q0, q1);
+                int kvh, ku, split, q0, q1;
+                w.item(a, i, kvh, ku, split, q0, q1);
                 if (q0 >= q1) continue;
-                ok = mbar_wait(bar(M_KEMPTY + kc % SK), ((kc / SK) & 1) ^ 1, ctl, a.status);
-                if (!ok) break;
-                const uint32_t kb = bar(M_KFULL + kc % SK), kd = k_slot(kc % SK);
-                mbar_expect_tx(kb, kTileBytes);
-                if (a.page_table) {
-                    const int page = a.page_table[kt];
-                    tma_load_4d(kd, &map_k, kb, 0, 0, kvh, page);
-                    tma_load_4d(kd + kPanel, &map_k, kb, 64, 0, kvh, page);
-                } else {
-                    tma_load_3d(kd, &map_k, kb, 0, kt * kTile, kvh);
-                    tma_load_3d(kd + kPanel, &map_k, kb, 64, kt * kTile, kvh);
+                for (int kt = 2 * ku; kt < min(2 * ku + 2, w.nkt); ++kt, ++kc) {
+                    ok = mbar_wait(bar(M_KEMPTY + kc % SK), ((kc / SK) & 1) ^ 1, ctl, a.status);
+                    if (!ok) break;
+                    const uint32_t kb = bar(M_KFULL + kc % SK), kd = k_slot(kc % SK);
+                    mbar_expect_tx(kb, kTileBytes);
+                    if (a.page_table) {
+                        const int page = a.page_table[kt];
+                        tma_load_4d(kd, &map_k, kb, 0, 0, kvh, page);
+                        tma_load_4d(kd + kPanel, &map_k, kb, 64, 0, kvh, page);
+                    } else {
+                        tma_load_3d(kd, &map_k, kb, 0, kt * kTile, kvh);
+                        tma_load_3d(kd + kPanel, &map_k, kb, 64, kt * kTile, kvh);
+                    }
                 }
-                ++kc;
+                if (!ok) break;
                 for (int q = q0; q < q1; ++q) {
                     if (kOne && held == kvh) break;
                     held = kvh;
@@ -166,37 +189,44 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         int kc = 0, qc = 0, jc = 0, held = -1;
         bool ok = true;
         for (int64_t i = i0; ok && i < i1; i += istep) {
-            int kvh, kt, split, q0, q1;
-            w.item(a, i, kvh, kt, split, q0, q1);
+            int kvh, ku, split, q0, q1;
+            w.item(a, i, kvh, ku, split, q0, q1);
             if (q0 >= q1) continue;
             if (kOne && held >= 0 && held != kvh) {          // the last head's query tile has been read
                 if (leader) tc_commit(bar(M_QEMPTY));
                 ++qc;
             }
-            ok = mbar_wait_warp(bar(M_KFULL + kc % SK), (kc / SK) & 1, ctl, a.status);
-            if (!ok) break;
-            const uint64_t kdesc = desc_kmajor(k_slot(kc % SK));
+            const int tiles = min(2, w.nkt - 2 * ku);
             for (int q = q0; q < q1; ++q, ++jc) {
-                if (!kOne || held != kvh) ok = mbar_wait_warp(bar(M_QFULL + qc % SQ), (qc / SQ) & 1, ctl, a.status);
+                // (what is not there to be waited for is asked for twice)
+                const Phase acc = {bar(M_DEMPTY + (jc & 1)), (uint32_t)((jc >> 1) & 1) ^ 1u};
+                const Phase k0 = q == q0 ? Phase{bar(M_KFULL + kc % SK), (uint32_t)(kc / SK) & 1u} : acc;
+                const Phase k1 = q == q0 && tiles == 2 ? Phase{bar(M_KFULL + (kc + 1) % SK), (uint32_t)((kc + 1) / SK) & 1u} : acc;
+                const Phase qt = !kOne || held != kvh ? Phase{bar(M_QFULL + qc % SQ), (uint32_t)(qc / SQ) & 1u} : acc;
                 held = kvh;
-                if (ok) ok = mbar_wait_warp(bar(M_DEMPTY + jc % kAccs), ((jc / kAccs) & 1) ^ 1, ctl, a.status);
+                const Phase all[4] = {acc, k0, k1, qt};
+                ok = mbar_wait4_warp(all, ctl, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t qdesc = desc_kmajor(q_slot(qc % SQ));
+#pragma unroll 1
+                for (int t = 0; t < tiles; ++t) {
+                    const uint64_t kdesc = desc_kmajor(k_slot((kc + t) % SK));
+                    const uint32_t d = tmem + (uint32_t)(jc & 1) * 256u + (uint32_t)t * 128u;
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint64_t off = (uint64_t)(((kk >> 2) * kPanel + (kk & 3) * 32) >> 4);
-                    if (leader) tc_mma(tmem + (uint32_t)(jc % kAccs) * 128u, kdesc + off, qdesc + off, idesc, kk > 0);
+                    for (int kk = 0; kk < 8; ++kk) {
+                        const uint64_t off = (uint64_t)(((kk >> 2) * kPanel + (kk & 3) * 32) >> 4);
+                        if (leader) tc_mma(d, kdesc + off, qdesc + off, idesc, kk > 0);
+                    }
+                    if (leader && q == q1 - 1) tc_commit(bar(M_KEMPTY + (kc + t) % SK));
                 }
-                if (leader) tc_commit(bar(M_DFULL + jc % kAccs));
+                if (leader) tc_commit(bar(M_DFULL + (jc & 1)));
                 if (!kOne) {
                     if (leader) tc_commit(bar(M_QEMPTY + qc % SQ));
                     ++qc;
                 }
             }
-            if (!ok) break;
-            if (leader) tc_commit(bar(M_KEMPTY + kc % SK));
-            ++kc;
+            kc += tiles;
         }
         // whatever made this warp leave its loop, tensor memory is released only after every MMA it issued has run
         if (leader) {
@@ -216,9 +246,9 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         int jc = 0;
         bool ok = true;
         for (int64_t i = i0; ok && i < i1; i += istep) {
-            int kvh, kt, split, q0, q1;
-            w.item(a, i, kvh, kt, split, q0, q1);
-            const int64_t key0 = (int64_t)kt * kTile;
+            int kvh, ku, split, q0, q1;
+            w.item(a, i, kvh, ku, split, q0, q1);
+            const int64_t key0 = (int64_t)ku * kUnit;
             for (int q = q0; q < q1; ++q, ++jc) {
                 if ((jc & 1) != warp - 2) continue;
                 float l[4];
@@ -233,8 +263,11 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 if (!ok) break;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) cols->neg[lane + 32 * k] = l[k] == -INFINITY ? -INFINITY : -l[k] * kLog2e;
-                // does every token see all of the key tile?  (without ranges known from the tile's first token)
-                bool some = true, part = ranged || key0 + kTile > P + (int64_t)(q * w.toks + 1) * a.self_rows;
+                // does every token see all of the keys?  (without ranges known from the tile's first token)
+                // (nor where a denominator is NaN: a pair's way through the multiply-add pipe would lose it)
+                bool some = true, part = ranged || key0 + kUnit > P + (int64_t)(q * w.toks + 1) * a.self_rows;
+                const bool odd = __any_sync(0xffffffffu, l[0] != l[0] || l[1] != l[1] || l[2] != l[2] || l[3] != l[3]);
+                part = part || odd;
                 if (part || biased) {
                     some = part = false;
 #pragma unroll
@@ -244,15 +277,15 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         float2 bias = both(0.f);
                         if (tok_of[k] < w.toks && tok < a.n) {
                             const RowRange seen = a.scored ? seen_rows(a.mods, tok, tok, P, L, a.self_rows) : RowRange{0, P + (int64_t)(tok + 1) * a.self_rows};
-                            const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kTile), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kTile);
+                            const int lo = (int)min(max(seen.begin - key0, (int64_t)0), (int64_t)kUnit), hi = (int)min(max(seen.end - key0, (int64_t)0), (int64_t)kUnit);
                             if (lo < hi) {
-                                sees = (uint32_t)lo | (uint32_t)hi << 8;
+                                sees = (uint32_t)lo | (uint32_t)hi << 16;
                                 some = true;
                             }
-                            part = part || lo > 0 || hi < kTile;
+                            part = part || odd || lo > 0 || hi < kUnit;
                             if (biased) bias = make_float2(a.mods.slopes[kvh * G + head_of[k]] * kLog2e, (float)(a.mods.pos0 + tok - key0));
                         }
-                        cols->seen[lane + 32 * k] = (uint16_t)sees;
+                        cols->seen[lane + 32 * k] = sees;
                         cols->bias[lane + 32 * k] = bias;
                     }
                     some = __any_sync(0xffffffffu, some);
@@ -267,124 +300,145 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
             }
         }
     } else {
-        // ------------------------------------------------------------------ exponentials: a thread per key
+        // ------------------------------------------------------------------ exponentials: a thread per key (kOne) or two
         const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-        const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16);
+        constexpr int NK = kOne ? 1 : 2;                 // keys of a thread: r of key tile t0, and of the next
+        const int t0 = kOne ? group & 1 : 0, turn = kOne ? group >> 1 : 0;
+        const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)t0 * 128u;
         const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
         const float2 sl2 = both(a.scale_log2);
         int jc = 0, sums = 0;
         bool ok = true;
         for (int64_t i = i0; ok && i < i1; i += istep) {
-            int kvh, kt, split, q0, q1;
-            w.item(a, i, kvh, kt, split, q0, q1);
-            const int64_t key0 = (int64_t)kt * kTile;
-            float2 acc0 = both(0.f), acc1 = both(0.f);
-            const int jc0 = jc;
+            int kvh, ku, split, q0, q1;
+            w.item(a, i, kvh, ku, split, q0, q1);
+            const int64_t key0 = (int64_t)ku * kUnit;
+            if (kOne && (jc & 1) != turn) { jc += q1 - q0; continue; }           // (kOne: an item is one job)
+            // the weight so far, called for ahead of the work
+            const bool last = w.splits == 1 && (kOne || group == 0);
+            float before[NK];
+#pragma unroll
+            for (int t = 0; t < NK; ++t) {
+                const int64_t key = key0 + (t0 + t) * kTile + r;
+                before[t] = last && a.mass_in && a.decay != 0.f && key < a.held ? a.mass_in[(int64_t)kvh * a.in_stride + key] : 0.f;
+            }
+            float2 acc[NK][2];
+#pragma unroll
+            for (int t = 0; t < NK; ++t) acc[t][0] = acc[t][1] = both(0.f);
             for (int q = q0; q < q1; ++q, ++jc) {
-                if (jc % kGroups != group) continue;
                 const Cols *cols = reinterpret_cast<const Cols *>(smem + kOffCols) + jc % kColSlots;
-                const uint32_t neg = base + kOffCols + (uint32_t)(jc % kColSlots) * (uint32_t)sizeof(Cols);
-                ok = mbar_wait(bar(M_CFULL + jc % kColSlots), (jc / kColSlots) & 1, ctl, a.status);
-                ok = __all_sync(0xffffffffu, ok);
+                const uint32_t col0 = base + kOffCols + (uint32_t)(jc % kColSlots) * (uint32_t)sizeof(Cols);
+                const Phase known = {bar(M_CFULL + jc % kColSlots), (uint32_t)(jc / kColSlots) & 1u}, full = {bar(M_DFULL + (jc & 1)), (uint32_t)(jc >> 1) & 1u};
+                const Phase all[4] = {known, full, known, full};
+                ok = mbar_wait4_warp(all, ctl, a.status);
                 if (!ok) break;
                 const bool some = *reinterpret_cast<const volatile int *>(&cols->some), part = *reinterpret_cast<const volatile int *>(&cols->part);
-                ok = mbar_wait(bar(M_DFULL + jc % kAccs), (jc / kAccs) & 1, ctl, a.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
                 tc_fence_after();
-                const uint32_t t_job = t_acc + (uint32_t)(jc % kAccs) * 128u;
-                // C columns from c0 on, their dot products in v
-                auto add = [&](auto v, int c0, auto ncol) {
-                    constexpr int C = decltype(ncol)::value;
-                    auto dot = [&](int c) { return make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])); };
+                const uint32_t t_job = t_acc + (uint32_t)(jc & 1) * 256u;
+                constexpr int C = 16;
+                // C columns from c0 on, their dot products with my keys in v
+                auto add = [&](uint32_t (&v)[NK][C], int c0) {
+                    auto dot = [&](int t, int c) { return make_float2(__uint_as_float(v[t][c]), __uint_as_float(v[t][c + 1])); };
                     int tier = 0;                // 0: no cap; 1, 2, 3: by the largest of my warp's scores (scores.cuh)
                     if (cap) {
                         float far = 0.f;
 #pragma unroll
-                        for (int c = 0; c < C; ++c) far = fmaxf(far, fabsf(__uint_as_float(v[c])));
+                        for (int t = 0; t < NK; ++t)
+#pragma unroll
+                            for (int c = 0; c < C; ++c) far = fmaxf(far, fabsf(__uint_as_float(v[t][c])));
                         tier = !__any_sync(0xffffffffu, far > a.mods.small_to) ? 1 : !__any_sync(0xffffffffu, far > a.mods.middle_to) ? 2 : 3;
                     }
                     if (tier == 2) {
 #pragma unroll
-                        for (int c = 0; c < C; c += 2) {
-                            const float2 y = cap_middle(a.mods, dot(c));
-                            v[c] = __float_as_uint(y.x);
-                            v[c + 1] = __float_as_uint(y.y);
-                        }
+                        for (int t = 0; t < NK; ++t)
+#pragma unroll
+                            for (int c = 0; c < C; c += 2) {
+                                const float2 y = cap_middle(a.mods, dot(t, c));
+                                v[t][c] = __float_as_uint(y.x);
+                                v[t][c + 1] = __float_as_uint(y.y);
+                            }
                     } else if (tier == 3) {
 #pragma unroll
-                        for (int c = 0; c < C; ++c) v[c] = __float_as_uint(cap_any(a.mods, __uint_as_float(v[c])));
+                        for (int t = 0; t < NK; ++t)
+#pragma unroll
+                            for (int c = 0; c < C; ++c) v[t][c] = __float_as_uint(cap_any(a.mods, __uint_as_float(v[t][c])));
                     }
-                    auto sum_up = [&](auto exponent) {
+                    // (kFma: every fourth pair of exponentials on the multiply-add pipe)
+                    auto sum_up = [&](auto exponent, auto fma) {
+                        constexpr bool kFma = decltype(fma)::value;
 #pragma unroll
                         for (int c = 0; c < C; c += 4) {
-                            float4 n4;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(n4.x), "=f"(n4.y), "=f"(n4.z), "=f"(n4.w) : "r"(neg + (uint32_t)(c0 + c) * 4u));
-                            const float2 y0 = exponent(c, make_float2(n4.x, n4.y)), y1 = exponent(c + 2, make_float2(n4.z, n4.w));
-                            acc0 = __fadd2_rn(acc0, make_float2(ex2(y0.x), ex2(y0.y)));
-                            acc1 = __fadd2_rn(acc1, make_float2(ex2(y1.x), ex2(y1.y)));
+                            float n4[4];
+                            lds128(col0 + (uint32_t)(c0 + c) * 4u, n4);
+#pragma unroll
+                            for (int t = 0; t < NK; ++t) {
+                                const float2 y0 = exponent(t, c, make_float2(n4[0], n4[1])), y1 = exponent(t, c + 2, make_float2(n4[2], n4[3]));
+                                acc[t][0] = __fadd2_rn(acc[t][0], make_float2(ex2(y0.x), ex2(y0.y)));
+                                acc[t][1] = __fadd2_rn(acc[t][1], kFma && (c & 4) ? exp2_fma(y1) : make_float2(ex2(y1.x), ex2(y1.y)));
+                            }
                         }
                     };
                     if (part || biased) {
                         const float2 by = cap ? both(1.f) : sl2;
-                        sum_up([&](int c, float2 n2) {
-                            float2 y = tier == 1 ? __ffma2_rn(dot(c), cap_small_over(a.mods, dot(c)), n2) : __ffma2_rn(dot(c), by, n2);
+                        sum_up([&](int t, int c, float2 n2) {
+                            float2 y = tier == 1 ? __ffma2_rn(dot(t, c), cap_small_over(a.mods, dot(t, c)), n2) : __ffma2_rn(dot(t, c), by, n2);
+                            const int at = (t0 + t) * kTile + r;
                             if (biased) {
-                                float2 b0, b1;
-                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b0.x), "=f"(b0.y), "=f"(b1.x), "=f"(b1.y)
-                                             : "r"(neg + (uint32_t)offsetof(Cols, bias) + (uint32_t)(c0 + c) * 8u));
-                                y.x = fmaf(-b0.x, fabsf(b0.y - (float)r), y.x);
-                                y.y = fmaf(-b1.x, fabsf(b1.y - (float)r), y.y);
+                                float b[4];
+                                lds128(col0 + (uint32_t)offsetof(Cols, bias) + (uint32_t)(c0 + c) * 8u, b);
+                                y.x = fmaf(-b[0], fabsf(b[1] - (float)at), y.x);
+                                y.y = fmaf(-b[2], fabsf(b[3] - (float)at), y.y);
                             }
                             if (part) {
-                                uint32_t s01;
-                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(s01) : "r"(neg + (uint32_t)offsetof(Cols, seen) + (uint32_t)(c0 + c) * 2u));
-                                const uint32_t s0 = s01 & 0xFFFFu, s1 = s01 >> 16;
-                                y.x = r >= (int)(s0 & 0xFFu) && r < (int)(s0 >> 8) ? y.x : -INFINITY;
-                                y.y = r >= (int)(s1 & 0xFFu) && r < (int)(s1 >> 8) ? y.y : -INFINITY;
+                                uint32_t s0, s1;
+                                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(s0), "=r"(s1) : "r"(col0 + (uint32_t)offsetof(Cols, seen) + (uint32_t)(c0 + c) * 4u));
+                                y.x = at >= (int)(s0 & 0xFFFFu) && at < (int)(s0 >> 16) ? y.x : -INFINITY;
+                                y.y = at >= (int)(s1 & 0xFFFFu) && at < (int)(s1 >> 16) ? y.y : -INFINITY;
                             }
                             return y;
-                        });
+                        }, std::false_type{});
                     } else if (tier == 0) {
-                        sum_up([&](int c, float2 n2) { return __ffma2_rn(dot(c), sl2, n2); });
+                        sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), sl2, n2); }, std::true_type{});
                     } else if (tier == 1) {
-                        sum_up([&](int c, float2 n2) { return __ffma2_rn(dot(c), cap_small_over(a.mods, dot(c)), n2); });
+                        sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), cap_small_over(a.mods, dot(t, c)), n2); }, std::true_type{});
                     } else {
-                        sum_up([&](int c, float2 n2) { return __fadd2_rn(dot(c), n2); });
+                        sum_up([&](int t, int c, float2 n2) { return __fadd2_rn(dot(t, c), n2); }, std::false_type{});
                     }
                 };
                 if (some) {
-                    constexpr int C = kOne ? 16 : 32;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < (kOne ? ncols : kTile); c0 += C) {
-                        uint32_t v[C];
+                    for (int c0 = kOne ? 0 : group * (kTile / kGroups); c0 < (kOne ? ncols : (group + 1) * (kTile / kGroups)); c0 += C) {
+                        uint32_t v[NK][C];
                         __syncwarp();
-                        if constexpr (kOne) KVF_TMEM_LD16(v, 0, t_job + c0);
-                        else KVF_TMEM_LD32(v, 0, t_job + c0);
+#pragma unroll
+                        for (int t = 0; t < NK; ++t) KVF_TMEM_LD16(v[t], 0, t_job + t * 128 + c0);
                         tmem_wait_ld();
-                        add(v, c0, std::integral_constant<int, C>{});
+                        add(v, c0);
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(bar(M_DEMPTY + jc % kAccs));
+                    mbar_arrive(bar(M_DEMPTY + (jc & 1)));
                     mbar_arrive(bar(M_CEMPTY + jc % kColSlots));
                 }
             }
             if (!ok) break;
-            const float2 acc = __fadd2_rn(acc0, acc1);
-            float sum = acc.x + acc.y;
-            if (kOne) {
-                if (jc == jc0 ? group != 0 : jc0 % kGroups != group) continue;           // the other group had the job
-            } else {
-                // the other groups' sums of the key go to the first
+            float sum[NK];
+#pragma unroll
+            for (int t = 0; t < NK; ++t) {
+                const float2 both_acc = __fadd2_rn(acc[t][0], acc[t][1]);
+                sum[t] = both_acc.x + both_acc.y;
+            }
+            if (!kOne) {
+                // the other groups' sums of the keys go to the first
                 ++sums;
                 if (group > 0) {
                     if (sums > 1) ok = mbar_wait(bar(M_TAKEN + quarter), (sums - 2) & 1, ctl, a.status);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    *reinterpret_cast<volatile float *>(&ctl->sums[group - 1][r]) = sum;
+#pragma unroll
+                    for (int t = 0; t < NK; ++t) *reinterpret_cast<volatile float *>(&ctl->sums[group - 1][t * kTile + r]) = sum[t];
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(M_SUM + quarter));
                     continue;
@@ -393,17 +447,18 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
 #pragma unroll
-                for (int o = 1; o < kGroups; ++o) sum += *reinterpret_cast<volatile float *>(&ctl->sums[o - 1][r]);
+                for (int t = 0; t < NK; ++t)
+#pragma unroll
+                    for (int o = 1; o < kGroups; ++o) sum[t] += *reinterpret_cast<volatile float *>(&ctl->sums[o - 1][t * kTile + r]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(M_TAKEN + quarter));
             }
-            const int64_t key = key0 + r;
-            if (key >= L) continue;
-            if (w.splits > 1) {
-                a.parts[((int64_t)split * a.Hkv + kvh) * L + key] = sum;
-            } else {
-                if (a.mass_in && a.decay != 0.f && key < a.held) sum = fmaf(a.decay, a.mass_in[(int64_t)kvh * a.in_stride + key], sum);
-                a.mass_out[(int64_t)kvh * a.out_stride + key] = sum;
+#pragma unroll
+            for (int t = 0; t < NK; ++t) {
+                const int64_t key = key0 + (t0 + t) * kTile + r;
+                if (key >= L) continue;
+                if (w.splits > 1) a.parts[((int64_t)split * a.Hkv + kvh) * L + key] = sum[t];
+                else a.mass_out[(int64_t)kvh * a.out_stride + key] = fmaf(a.decay, before[t], sum[t]);
             }
         }
     }
@@ -561,14 +616,15 @@ cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CU
     MassWork w;
     w.toks = mass_tile_tokens(a.G);
     w.nkt = (int)((a.rows + kTile - 1) / kTile);
+    w.nku = (w.nkt + 1) / 2;
     w.nq = (a.n + w.toks - 1) / w.toks;
     w.one = w.nq == 1;
-    const int64_t units = (int64_t)a.Hkv * w.nkt;
-    // Splits of the query tiles: as many as fill the waves of CTAs best (a fifth of a tile for what an item costs besides)
+    const int64_t units = (int64_t)a.Hkv * w.nku;
+    // Splits of the query tiles: as many as fill the waves of CTAs best (a tile for what an item costs besides)
     w.splits = 1;
     double least = 0.0;
-    for (int sp = 1; sp <= w.nq && sp <= 8 && (int64_t)sp * a.Hkv * a.rows <= a.parts_cap; ++sp) {
-        const double waves = (double)((units * sp + a.sms - 1) / a.sms), t = waves * ((double)w.nq / sp + 0.2) + (sp > 1 ? 2.0 : 0.0);
+    for (int sp = 1; sp <= w.nq && sp <= 16 && (int64_t)sp * a.Hkv * a.rows <= a.parts_cap; ++sp) {
+        const double waves = (double)((units * sp + a.sms - 1) / a.sms), t = waves * ((double)w.nq / sp + 1.0) + (sp > 1 ? 2.0 : 0.0);
         if (sp == 1 || t < least) { least = t; w.splits = sp; }
     }
     w.items = units * w.splits;

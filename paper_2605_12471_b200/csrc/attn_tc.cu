@@ -164,37 +164,6 @@ __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr) {
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// One go at several barriers: the answers are asked for back to back and looked at together (an answer takes 150 - 200 cycles to
-// come even when it is yes).
-struct Phase {
-    uint32_t bar, parity;
-};
-__device__ __forceinline__ bool mbar_try_wait4(const Phase (&w)[4]) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p, q, r, s;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %9;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4, %9;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 r, [%5], %6, %9;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 s, [%7], %8, %9;\n\t"
-        "and.pred p, p, q;\n\t"
-        "and.pred r, r, s;\n\t"
-        "and.pred p, p, r;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(w[0].bar), "r"(w[0].parity), "r"(w[1].bar), "r"(w[1].parity), "r"(w[2].bar), "r"(w[2].parity),
-          "r"(w[3].bar), "r"(w[3].parity), "r"(kSuspendHintNs) : "memory");
-    return ok;
-}
-__device__ __forceinline__ bool mbar_wait4_warp(const Phase (&w)[4], Ctl *ctl, int *status) {
-    bool ok = mbar_try_wait4(w);
-    if (!ok) {
-        ok = true;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) ok = ok && mbar_wait(w[k].bar, w[k].parity, ctl, status);
-    }
-    return __all_sync(0xffffffffu, ok);
-}
-
 // Instruction descriptor: D fp32, A and B bf16, M = 128, N = 128; bit 16 = B is MN-major.
 constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 constexpr uint32_t kIdescPV = kIdescQK | (1u << 16);
