@@ -22,7 +22,7 @@ namespace kvf {
 namespace {
 
 // ---- tensor cores
-constexpr int kTile = 128, kD = 128, kUnit = 2 * kTile;      // keys of a tile, of an item
+constexpr int kTile = 128, kUnit = 2 * kTile;      // keys of a tile, of an item
 constexpr uint32_t kPanel = 128 * 128, kTileBytes = 2 * kPanel;
 constexpr int kGroups = 4;                     // groups of four warps of exponentials (a warp has a quarter of the lanes)
 constexpr int kTcThreads = 128 + kGroups * 128;        // warp 0 TMA, warp 1 MMA, warps 2 and 3 what is to be known of the columns, the others exponentials
@@ -91,8 +91,8 @@ struct MassWork {
     }
 };
 
-// kOne: the chunk is one query tile of `ncols` columns (a multiple of 16).
-template <bool kOne>
+// kOne: the chunk is one query tile of `ncols` columns (a multiple of 16).  kCap: scores are capped.
+template <bool kOne, bool kCap>
 __global__ void __launch_bounds__(kTcThreads, 1)
 mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
     constexpr int SK = kOne ? 5 : 4, SQ = kOne ? 1 : 2;
@@ -305,7 +305,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         constexpr int NK = kOne ? 1 : 2;                 // keys of a thread: r of key tile t0, and of the next
         const int t0 = kOne ? group & 1 : 0, turn = kOne ? group >> 1 : 0;
         const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)t0 * 128u;
-        const bool cap = a.scored && a.mods.cap_out > 0.f, biased = a.scored && a.mods.slopes;
+        const bool biased = a.scored && a.mods.slopes;
         const float2 sl2 = both(a.scale_log2);
         int jc = 0, sums = 0;
         bool ok = true;
@@ -336,84 +336,75 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 tc_fence_after();
                 const uint32_t t_job = t_acc + (uint32_t)(jc & 1) * 256u;
                 constexpr int C = 16;
-                // C columns from c0 on, their dot products with my keys in v
-                auto add = [&](uint32_t (&v)[NK][C], int c0) {
-                    auto dot = [&](int t, int c) { return make_float2(__uint_as_float(v[t][c]), __uint_as_float(v[t][c + 1])); };
-                    int tier = 0;                // 0: no cap; 1, 2, 3: by the largest of my warp's scores (scores.cuh)
-                    if (cap) {
-                        float far = 0.f;
+                const int from = kOne ? 0 : group * (kTile / kGroups), to = kOne ? ncols : from + kTile / kGroups;
+                if (some && (part || biased)) {
+                    // (a way of its own, behind the branch of a whole job: beside the other it cost that 60 us of 340 in a launch whose jobs
+                    // hardly ever take it)
+#pragma unroll 1
+                    for (int c0 = from; c0 < to; c0 += C)
 #pragma unroll
-                        for (int t = 0; t < NK; ++t)
+                        for (int t = 0; t < NK; ++t) {
+                            uint32_t v[C];
+                            __syncwarp();
+                            KVF_TMEM_LD16(v, 0, t_job + t * 128 + c0);
+                            tmem_wait_ld();
+                            const int at = (t0 + t) * kTile + r;
 #pragma unroll
-                            for (int c = 0; c < C; ++c) far = fmaxf(far, fabsf(__uint_as_float(v[t][c])));
-                        tier = !__any_sync(0xffffffffu, far > a.mods.small_to) ? 1 : !__any_sync(0xffffffffu, far > a.mods.middle_to) ? 2 : 3;
-                    }
-                    if (tier == 2) {
-#pragma unroll
-                        for (int t = 0; t < NK; ++t)
-#pragma unroll
-                            for (int c = 0; c < C; c += 2) {
-                                const float2 y = cap_middle(a.mods, dot(t, c));
-                                v[t][c] = __float_as_uint(y.x);
-                                v[t][c + 1] = __float_as_uint(y.y);
-                            }
-                    } else if (tier == 3) {
-#pragma unroll
-                        for (int t = 0; t < NK; ++t)
-#pragma unroll
-                            for (int c = 0; c < C; ++c) v[t][c] = __float_as_uint(cap_any(a.mods, __uint_as_float(v[t][c])));
-                    }
-                    // (kFma: every fourth pair of exponentials on the multiply-add pipe)
-                    auto sum_up = [&](auto exponent, auto fma) {
-                        constexpr bool kFma = decltype(fma)::value;
-#pragma unroll
-                        for (int c = 0; c < C; c += 4) {
-                            float n4[4];
-                            lds128(col0 + (uint32_t)(c0 + c) * 4u, n4);
-#pragma unroll
-                            for (int t = 0; t < NK; ++t) {
-                                const float2 y0 = exponent(t, c, make_float2(n4[0], n4[1])), y1 = exponent(t, c + 2, make_float2(n4[2], n4[3]));
-                                acc[t][0] = __fadd2_rn(acc[t][0], make_float2(ex2(y0.x), ex2(y0.y)));
-                                acc[t][1] = __fadd2_rn(acc[t][1], kFma && (c & 4) ? exp2_fma(y1) : make_float2(ex2(y1.x), ex2(y1.y)));
+                            for (int c = 0; c < C; ++c) {
+                                const float s = __uint_as_float(v[c]);
+                                const volatile Cols *col = cols;
+                                float y = (kCap ? cap_any(a.mods, s) : s * sl2.x) + col->neg[c0 + c];
+                                if (biased) y = fmaf(-col->bias[c0 + c].x, fabsf(col->bias[c0 + c].y - (float)at), y);
+                                const uint32_t sees = col->seen[c0 + c];
+                                acc[t][0].x += at >= (int)(sees & 0xFFFFu) && at < (int)(sees >> 16) ? ex2(y) : 0.f;
                             }
                         }
-                    };
-                    if (part || biased) {
-                        const float2 by = cap ? both(1.f) : sl2;
-                        sum_up([&](int t, int c, float2 n2) {
-                            float2 y = tier == 1 ? __ffma2_rn(dot(t, c), cap_small_over(a.mods, dot(t, c)), n2) : __ffma2_rn(dot(t, c), by, n2);
-                            const int at = (t0 + t) * kTile + r;
-                            if (biased) {
-                                float b[4];
-                                lds128(col0 + (uint32_t)offsetof(Cols, bias) + (uint32_t)(c0 + c) * 8u, b);
-                                y.x = fmaf(-b[0], fabsf(b[1] - (float)at), y.x);
-                                y.y = fmaf(-b[2], fabsf(b[3] - (float)at), y.y);
-                            }
-                            if (part) {
-                                uint32_t s0, s1;
-                                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(s0), "=r"(s1) : "r"(col0 + (uint32_t)offsetof(Cols, seen) + (uint32_t)(c0 + c) * 4u));
-                                y.x = at >= (int)(s0 & 0xFFFFu) && at < (int)(s0 >> 16) ? y.x : -INFINITY;
-                                y.y = at >= (int)(s1 & 0xFFFFu) && at < (int)(s1 >> 16) ? y.y : -INFINITY;
-                            }
-                            return y;
-                        }, std::false_type{});
-                    } else if (tier == 0) {
-                        sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), sl2, n2); }, std::true_type{});
-                    } else if (tier == 1) {
-                        sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), cap_small_over(a.mods, dot(t, c)), n2); }, std::true_type{});
-                    } else {
-                        sum_up([&](int t, int c, float2 n2) { return __fadd2_rn(dot(t, c), n2); }, std::false_type{});
-                    }
-                };
-                if (some) {
+                } else if (some) {
 #pragma unroll 1
-                    for (int c0 = kOne ? 0 : group * (kTile / kGroups); c0 < (kOne ? ncols : (group + 1) * (kTile / kGroups)); c0 += C) {
+                    for (int c0 = from; c0 < to; c0 += C) {
                         uint32_t v[NK][C];
                         __syncwarp();
 #pragma unroll
                         for (int t = 0; t < NK; ++t) KVF_TMEM_LD16(v[t], 0, t_job + t * 128 + c0);
                         tmem_wait_ld();
-                        add(v, c0);
+                        auto dot = [&](int t, int c) { return make_float2(__uint_as_float(v[t][c]), __uint_as_float(v[t][c + 1])); };
+                        // (every fourth pair of exponentials goes through the multiply-add pipe)
+                        auto sum_up = [&](auto exponent) {
+#pragma unroll
+                            for (int c = 0; c < C; c += 4) {
+                                float n4[4];
+                                lds128(col0 + (uint32_t)(c0 + c) * 4u, n4);
+#pragma unroll
+                                for (int t = 0; t < NK; ++t) {
+                                    const float2 y0 = exponent(t, c, make_float2(n4[0], n4[1])), y1 = exponent(t, c + 2, make_float2(n4[2], n4[3]));
+                                    acc[t][0] = __fadd2_rn(acc[t][0], make_float2(ex2(y0.x), ex2(y0.y)));
+                                    acc[t][1] = __fadd2_rn(acc[t][1], c & 4 ? exp2_fma(y1) : make_float2(ex2(y1.x), ex2(y1.y)));
+                                }
+                            }
+                        };
+                        if constexpr (kCap) {
+                            float far = 0.f;
+#pragma unroll
+                            for (int t = 0; t < NK; ++t)
+#pragma unroll
+                                for (int c = 0; c < C; ++c) far = fmaxf(far, fabsf(__uint_as_float(v[t][c])));
+                            if (!__any_sync(0xffffffffu, far > a.mods.small_to)) {
+                                sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), cap_small_over(a.mods, dot(t, c)), n2); });
+                            } else {
+                                const bool middle = !__any_sync(0xffffffffu, far > a.mods.middle_to);
+#pragma unroll
+                                for (int t = 0; t < NK; ++t)
+#pragma unroll
+                                    for (int c = 0; c < C; c += 2) {
+                                        const float2 y = middle ? cap_middle(a.mods, dot(t, c)) : make_float2(cap_any(a.mods, dot(t, c).x), cap_any(a.mods, dot(t, c).y));
+                                        v[t][c] = __float_as_uint(y.x);
+                                        v[t][c + 1] = __float_as_uint(y.y);
+                                    }
+                                sum_up([&](int t, int c, float2 n2) { return __fadd2_rn(dot(t, c), n2); });
+                            }
+                        } else {
+                            sum_up([&](int t, int c, float2 n2) { return __ffma2_rn(dot(t, c), sl2, n2); });
+                        }
                     }
                 }
                 tc_fence_before();
@@ -630,7 +621,8 @@ cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CU
     w.items = units * w.splits;
     if (w.items >= (int64_t)1 << 31) return cudaErrorInvalidValue;          // (2^24 tiles of 128 rows for each of 16 heads, and beyond)
     const int ncols = w.one ? (a.n * a.G + 15) / 16 * 16 : kTile;
-    auto kernel = w.one ? mass_tc_kernel<true> : mass_tc_kernel<false>;
+    const bool cap = a.scored && a.mods.cap_out > 0.f;
+    auto kernel = w.one ? (cap ? mass_tc_kernel<true, true> : mass_tc_kernel<true, false>) : cap ? mass_tc_kernel<false, true> : mass_tc_kernel<false, false>;
     cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(kernel), (int)kMassSmem);
     if (e != cudaSuccess) return e;
     const int64_t ctas = w.items < a.sms ? w.items : a.sms;

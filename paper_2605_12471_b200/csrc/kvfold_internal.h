@@ -139,8 +139,8 @@ struct RopeAppendArgs {
 // s - slope[head] * |position of the token - row|; token i sees rows [first[i], end[i]).
 struct ScoreMods {
     float cap_in, cap_out;           // scale / softcap and softcap * log2(e) (cap_out = 0: no cap)
-    float small_to;                  // dot products up to this go by small[]: cap_out * tanh(x) = s * (small[0] + small[1] s^2 + small[2] s^4)
-    float small[3];                  // (s the dot product itself; see scores.cuh)
+    float small_to;                  // dot products up to this go by small[]: cap_out * tanh(x) = s * (small[0] + ... + small[3] s^6)
+    float small[4];                  // (s the dot product itself; see scores.cuh)
     float middle_to;                 // ... up to this by middle[]: x * (middle[0] + ... + middle[4] x^8), x = cap_in * s
     float middle[5];
     const float *slopes;             // device [H] or null

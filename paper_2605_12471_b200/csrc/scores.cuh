@@ -1,6 +1,7 @@
 // What the kernels of scored steps share: the rows a token sees, and the cap on a score (kvf_scores).
 #pragma once
 #include <limits.h>
+#include <math.h>
 
 #include "kvfold_internal.h"
 
@@ -23,18 +24,18 @@ __device__ __forceinline__ RowRange seen_rows(const ScoreMods &m, int64_t at, in
 
 // The cap, softcap * log2(e) * tanh(x) with x = scale / softcap * (q . k).  The special-function unit is what a softmax on the tensor
 // cores is short of, so that most scores go through multiply-adds: tanh(x) / x as a polynomial in x^2, of least relative error
-// over |x| <= 0.2 (three terms, 1.1e-7) and |x| <= 0.75 (five, 5.7e-7); coefficients by the exchange algorithm of Remez.  Beyond,
+// over |x| <= 0.5 (four terms, 5.5e-7) and |x| <= 0.75 (five, 5.7e-7); coefficients by the exchange algorithm of Remez.  Beyond,
 // and where one score of a warp's tile lies there, 1 - 2 / (1 + e^2x), whose error of 2^-22 is one of the cap.
-constexpr float kSmallX = 0.2f, kMiddleX = 0.75f;
-constexpr double kSmallTanh[3] = {0.9999998947912137, -0.33328590898391885, 0.13015407544114974};
+constexpr float kSmallX = 0.5f, kMiddleX = 0.75f;
+constexpr double kSmallTanh[4] = {0.9999994557708787, -0.33326317935743466, 0.13190296601601936, -0.044402226090620216};
 constexpr double kMiddleTanh[5] = {0.9999994349238549, -0.33328251532272035, 0.13258983219087364, -0.050056302629619055, 0.012929632363192806};
 inline void set_cap(ScoreMods &m, double scale, double softcap) {
     const double in = scale / softcap, out = softcap * 1.4426950408889634;
     m.cap_in = (float)in;
     m.cap_out = (float)out;
-    // (powers of `in` below fp32's range, under caps of a million and more: the middle polynomial alone, which does without)
-    m.small_to = in > 1e-7 ? (float)(kSmallX / in) : 0.f;
-    for (int i = 0; i < 3; ++i) m.small[i] = (float)(kSmallTanh[i] * out * in * (i > 0 ? in * in : 1.0) * (i > 1 ? in * in : 1.0));
+    // (powers of `in` below fp32's range, under caps of a thousand times the usual: the middle polynomial alone, which does without)
+    m.small_to = in > 1e-4 ? (float)(kSmallX / in) : 0.f;
+    for (int i = 0; i < 4; ++i) m.small[i] = (float)(kSmallTanh[i] * out * pow(in, 2 * i + 1));
     m.middle_to = (float)(kMiddleX / in);
     for (int i = 0; i < 5; ++i) m.middle[i] = (float)(kMiddleTanh[i] * out);
 }
@@ -50,7 +51,7 @@ __device__ __forceinline__ float2 cap_middle(const ScoreMods &m, float2 s) {
 // (s * cap_small_over is the score)
 __device__ __forceinline__ float2 cap_small_over(const ScoreMods &m, float2 s) {
     const float2 u = __fmul2_rn(s, s);
-    return __ffma2_rn(u, __ffma2_rn(u, both(m.small[2]), both(m.small[1])), both(m.small[0]));
+    return __ffma2_rn(u, __ffma2_rn(u, __ffma2_rn(u, both(m.small[3]), both(m.small[2])), both(m.small[1])), both(m.small[0]));
 }
 __device__ __forceinline__ float cap_any(const ScoreMods &m, float s) {
     float e, r;
