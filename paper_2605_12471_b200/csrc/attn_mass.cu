@@ -36,7 +36,7 @@ struct __align__(16) Cols {                    // what the exponentials need to 
     int some, part;                            // does any column see a key of the item; may one not see all of them
     int pad[2];
 };
-enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 2, M_DFULL = M_QEMPTY + 2, M_DEMPTY = M_DFULL + 2,
+enum { M_KFULL = 0, M_KEMPTY = M_KFULL + 5, M_QFULL = M_KEMPTY + 5, M_QEMPTY = M_QFULL + 4, M_DFULL = M_QEMPTY + 4, M_DEMPTY = M_DFULL + 2,
        M_SUM = M_DEMPTY + 2, M_TAKEN = M_SUM + 4, M_DRAIN = M_TAKEN + 4, M_CFULL, M_CEMPTY = M_CFULL + kColSlots, M_COUNT = M_CEMPTY + kColSlots };
 struct MassCtl {
     unsigned long long bars[M_COUNT];
@@ -96,9 +96,10 @@ template <bool kOne, bool kCap>
 __global__ void __launch_bounds__(kTcThreads, 1)
 mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k) {
     constexpr int SK = kOne ? 5 : 4, SQ = kOne ? 1 : 2;
-    // Many query tiles: all groups share a job, each a quarter of its columns for both key tiles (a thread has two keys, and what it
-    // reads of a column serves both).  One: two groups, one for each key tile, take every other job.
-    constexpr int kTurns = kOne ? 2 : 1, kWarpsOfJob = 16 / kTurns;
+    // Two groups share a job and the two pairs of groups take the jobs in turn, so that one pair's exponentials run while the other waits for
+    // its scores (all four on each job: 289 us instead of 271).  Many query tiles: a group has half of the job's columns for both key
+    // tiles (a thread has two keys, and what it reads of a column serves both).  One: all columns for one key tile.
+    constexpr int kTurns = 2, kWarpsOfJob = 16 / kTurns;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - smem_u32(smem_raw));
@@ -209,8 +210,9 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t qdesc = desc_kmajor(q_slot(qc % SQ));
-#pragma unroll 1
-                for (int t = 0; t < tiles; ++t) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (t >= tiles) break;
                     const uint64_t kdesc = desc_kmajor(k_slot((kc + t) % SK));
                     const uint32_t d = tmem + (uint32_t)(jc & 1) * 256u + (uint32_t)t * 128u;
 #pragma unroll
@@ -303,7 +305,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
         // ------------------------------------------------------------------ exponentials: a thread per key (kOne) or two
         const int group = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         constexpr int NK = kOne ? 1 : 2;                 // keys of a thread: r of key tile t0, and of the next
-        const int t0 = kOne ? group & 1 : 0, turn = kOne ? group >> 1 : 0;
+        const int t0 = kOne ? group & 1 : 0, turn = group >> 1;
         const uint32_t t_acc = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)t0 * 128u;
         const bool biased = a.scored && a.mods.slopes;
         const float2 sl2 = both(a.scale_log2);
@@ -326,17 +328,23 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
 #pragma unroll
             for (int t = 0; t < NK; ++t) acc[t][0] = acc[t][1] = both(0.f);
             for (int q = q0; q < q1; ++q, ++jc) {
+                if (!kOne && (jc & 1) != turn) continue;
                 const Cols *cols = reinterpret_cast<const Cols *>(smem + kOffCols) + jc % kColSlots;
                 const uint32_t col0 = base + kOffCols + (uint32_t)(jc % kColSlots) * (uint32_t)sizeof(Cols);
                 const Phase known = {bar(M_CFULL + jc % kColSlots), (uint32_t)(jc / kColSlots) & 1u}, full = {bar(M_DFULL + (jc & 1)), (uint32_t)(jc >> 1) & 1u};
-                const Phase all[4] = {known, full, known, full};
-                ok = mbar_wait4_warp(all, ctl, a.status);
+                ok = mbar_wait(known.bar, known.parity, ctl, a.status) && mbar_wait(full.bar, full.parity, ctl, a.status);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const bool some = *reinterpret_cast<const volatile int *>(&cols->some), part = *reinterpret_cast<const volatile int *>(&cols->part);
                 tc_fence_after();
                 const uint32_t t_job = t_acc + (uint32_t)(jc & 1) * 256u;
-                constexpr int C = 16;
-                const int from = kOne ? 0 : group * (kTile / kGroups), to = kOne ? ncols : from + kTile / kGroups;
+                constexpr int C = kOne ? 16 : 32;
+                auto given_back = [&]() {            // my part of the accumulators
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(M_DEMPTY + (jc & 1)));
+                };
+                const int from = kOne ? 0 : (group & 1) * (kTile / 2), to = kOne ? ncols : from + kTile / 2;
                 if (some && (part || biased)) {
                     // (a way of its own, behind the branch of a whole job: beside the other it cost that 60 us of 340 in a launch whose jobs
                     // hardly ever take it)
@@ -346,7 +354,8 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         for (int t = 0; t < NK; ++t) {
                             uint32_t v[C];
                             __syncwarp();
-                            KVF_TMEM_LD16(v, 0, t_job + t * 128 + c0);
+                            if constexpr (kOne) KVF_TMEM_LD16(v, 0, t_job + t * 128 + c0);
+                            else KVF_TMEM_LD32(v, 0, t_job + t * 128 + c0);
                             tmem_wait_ld();
                             const int at = (t0 + t) * kTile + r;
 #pragma unroll
@@ -365,10 +374,16 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         uint32_t v[NK][C];
                         __syncwarp();
 #pragma unroll
-                        for (int t = 0; t < NK; ++t) KVF_TMEM_LD16(v[t], 0, t_job + t * 128 + c0);
+                        for (int t = 0; t < NK; ++t) {
+                            if constexpr (kOne) KVF_TMEM_LD16(v[t], 0, t_job + t * 128 + c0);
+                            else KVF_TMEM_LD32(v[t], 0, t_job + t * 128 + c0);
+                        }
                         tmem_wait_ld();
+                        // (many query tiles: all that is left of the job is in registers now)
+                        if (!kOne && c0 + C == to) given_back();
                         auto dot = [&](int t, int c) { return make_float2(__uint_as_float(v[t][c]), __uint_as_float(v[t][c + 1])); };
-                        // (every fourth pair of exponentials goes through the multiply-add pipe)
+                        // (every fourth pair of exponentials goes through the multiply-add pipe, 286 -> 271 us; not under a cap, whose
+                        // polynomials fill that pipe, 138 against 126)
                         auto sum_up = [&](auto exponent) {
 #pragma unroll
                             for (int c = 0; c < C; c += 4) {
@@ -378,7 +393,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                                 for (int t = 0; t < NK; ++t) {
                                     const float2 y0 = exponent(t, c, make_float2(n4[0], n4[1])), y1 = exponent(t, c + 2, make_float2(n4[2], n4[3]));
                                     acc[t][0] = __fadd2_rn(acc[t][0], make_float2(ex2(y0.x), ex2(y0.y)));
-                                    acc[t][1] = __fadd2_rn(acc[t][1], c & 4 ? exp2_fma(y1) : make_float2(ex2(y1.x), ex2(y1.y)));
+                                    acc[t][1] = __fadd2_rn(acc[t][1], !kCap && (c & 4) ? exp2_fma(y1) : make_float2(ex2(y1.x), ex2(y1.y)));
                                 }
                             }
                         };
@@ -407,12 +422,9 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                         }
                     }
                 }
-                tc_fence_before();
+                if (kOne || !some || part || biased) given_back();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(M_DEMPTY + (jc & 1)));
-                    mbar_arrive(bar(M_CEMPTY + jc % kColSlots));
-                }
+                if (lane == 0) mbar_arrive(bar(M_CEMPTY + jc % kColSlots));
             }
             if (!ok) break;
             float sum[NK];
