@@ -15,7 +15,9 @@
 //
 // Move.  Rows are copied 16 bytes a thread, K and V rows of a KV head in one launch, eight loads in flight a thread; bound by memory
 // (two reads and two writes of every row kept).
-#include <algorithm>
+#include <mutex>
+#include <utility>
+#include <vector>
 
 #include "kvfold_internal.h"
 #include "sm100_ptx.cuh"
@@ -26,12 +28,13 @@ namespace {
 constexpr int kSelectThreads = 1024;
 constexpr int kBins = 2048;
 constexpr int kHeldKeys = 49152;                     // keys of a CTA's range in shared memory
+constexpr int64_t kOneCta = 4096, kEightCtas = 32768;  // candidates up to which a KV head gets one CTA, eight
 
 struct SelectShared {
     uint32_t hist[3][kBins];
     uint32_t scan[kSelectThreads / 32];
     uint32_t found_bin, found_above;                 // bin that the wanted key lies in, keys above that bin
-    uint32_t counts[2];                              // of this CTA's range: keys above the wanted key, keys equal to it
+    __align__(8) uint32_t counts[2];                              // of this CTA's range: keys above the wanted key, keys equal to it
     uint32_t warp_gt[kSelectThreads / 32], warp_eq[kSelectThreads / 32];
 };
 
@@ -41,20 +44,25 @@ __device__ __forceinline__ uint32_t key_of(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t peer_u32(const uint32_t *p, uint32_t rank) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_smem(smem_u32(p), rank)) : "memory");
+// (No "memory": loads of one and the same phase may be in flight together.  What separates the phases is volatile too.)
+__device__ __forceinline__ uint2 peer_pair(const uint32_t *p, uint32_t rank) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(peer_smem(smem_u32(p), rank)));
     return v;
 }
 
-// (kHeld: the range's keys stay in shared memory)
-template <bool kHeld>
-__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const EvictArgs a, const int ctas) {
+// kCtas: CTAs of a cluster.  kHeld: the range's keys stay in shared memory.
+template <bool kHeld, int kCtas>
+__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const EvictArgs a) {
+    constexpr int ctas = kCtas;
+    auto meet = [&]() {
+        if constexpr (kCtas > 1) cluster_sync_all();
+    };
     extern __shared__ __align__(16) uint8_t smem_raw[];
     SelectShared &sh = *reinterpret_cast<SelectShared *>(smem_raw);
     uint32_t *held = reinterpret_cast<uint32_t *>(smem_raw + sizeof(SelectShared));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = cluster_cta_rank();
+    const uint32_t rank = kCtas > 1 ? cluster_cta_rank() : 0u;
     const int g = blockIdx.x / ctas;
     const float *mass = a.mass + (int64_t)g * a.mass_stride;
     int32_t *kept = a.kept + (int64_t)g * a.budget;
@@ -85,26 +93,46 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : kBins;
         uint32_t *hist = sh.hist[pass];
-        for (int i = tid; i < mine; i += kSelectThreads) {
-            uint32_t k;
-            if (kHeld && pass == 0) {
-                k = key_of(w0[i]);
-                held[i] = k;
-            } else {
-                k = key_at(i);
+        if (pass == 0) {
+            // (eight loads in flight a thread)
+            for (int i = tid; i < mine; i += 8 * kSelectThreads) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = i + e * kSelectThreads < mine ? w0[i + e * kSelectThreads] : 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (i + e * kSelectThreads >= mine) break;
+                    const uint32_t k = key_of(x[e]);
+                    if (kHeld) held[i + e * kSelectThreads] = k;
+                    atomicAdd(&hist[k >> 21], 1u);
+                }
             }
-            const bool agrees = pass == 0 || (pass == 1 ? k >> 21 == known : k >> 10 == known);
-            if (agrees) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+        } else {
+            const int above_shift = pass == 1 ? 21 : 10;
+#pragma unroll 4
+            for (int i = tid; i < mine; i += kSelectThreads) {
+                const uint32_t k = key_at(i);
+                if (k >> above_shift == known) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+            }
         }
         __syncthreads();
-        cluster_sync_all();              // everybody's histogram is complete (and stays: the next pass has another)
+        meet();                          // everybody's histogram is complete (and stays: the next pass has another)
         // Bins from the top down, two a thread: thread t has bins top - 2 t and top - 2 t - 1.
         const int b0 = bins - 1 - 2 * tid;
         uint32_t c0 = 0u, c1 = 0u;
         if (b0 > 0) {
-            for (int r = 0; r < ctas; ++r) {
-                c0 += peer_u32(&hist[b0], (uint32_t)r);
-                c1 += peer_u32(&hist[b0 - 1], (uint32_t)r);
+            if constexpr (kCtas == 1) {
+                c0 = hist[b0];
+                c1 = hist[b0 - 1];
+            } else {
+                uint2 got[kCtas];
+#pragma unroll
+                for (int r = 0; r < kCtas; ++r) got[r] = peer_pair(&hist[b0 - 1], (uint32_t)r);
+#pragma unroll
+                for (int r = 0; r < kCtas; ++r) {
+                    c0 += got[r].y;
+                    c1 += got[r].x;
+                }
             }
         }
         uint32_t sum = c0 + c1;
@@ -163,11 +191,18 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
         if (lane == 31) { sh.counts[0] = x; sh.counts[1] = y; }
     }
     __syncthreads();
-    cluster_sync_all();
+    meet();
     uint32_t gt0 = sh.warp_gt[warp], eq0 = sh.warp_eq[warp];             // of rows below my warp's piece
-    for (uint32_t r = 0; r < rank; ++r) {
-        gt0 += peer_u32(&sh.counts[0], r);
-        eq0 += peer_u32(&sh.counts[1], r);
+    if constexpr (kCtas > 1) {
+        uint2 got[kCtas];
+#pragma unroll
+        for (int r = 0; r < kCtas; ++r) got[r] = peer_pair(sh.counts, (uint32_t)r);
+#pragma unroll
+        for (int r = 0; r < kCtas; ++r)
+            if (r < (int)rank) {
+                gt0 += got[r].x;
+                eq0 += got[r].y;
+            }
     }
     if (want > 0)
         for (int i = s0; i < s1; i += 32) {
@@ -185,7 +220,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
             eq0 += __popc(be);
         }
     __syncthreads();
-    cluster_sync_all();                  // nobody leaves while a partner may still read its counts
+    meet();                              // nobody leaves while a partner may still read its counts
 }
 
 constexpr int kMoveThreads = 256, kMoveItems = 8;
@@ -235,20 +270,55 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
 
 }  // namespace
 
+// Clusters of that many CTAs the device holds at once (queried once per device).
+template <int kCtas>
+static int select_clusters() {
+    static std::mutex mu;
+    static std::vector<std::pair<int, int>> seen;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    std::lock_guard<std::mutex> lock(mu);
+    for (auto &d : seen)
+        if (d.first == dev) return d.second;
+    auto kernel = evict_select_kernel<true, kCtas>;
+    const size_t most = sizeof(SelectShared) + (size_t)kHeldKeys * 4;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kCtas);
+    cfg.blockDim = dim3(kSelectThreads);
+    cfg.dynamicSmemBytes = most;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCtas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if ((kCtas > 8 && (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+                       cudaFuncSetAttribute(evict_select_kernel<false, kCtas>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) ||
+        raise_smem_limit_once(reinterpret_cast<const void *>(kernel), (int)most) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        clusters = 0;
+    }
+    seen.push_back({dev, clusters});
+    return clusters;
+}
+
+template <int kCtas>
+static cudaError_t launch_select(const EvictArgs &a, cudaStream_t s) {
+    const int64_t m = a.rows - a.n_sink - a.n_recent, per = (m + kCtas - 1) / kCtas;
+    const bool held = per <= kHeldKeys;
+    auto select = held ? evict_select_kernel<true, kCtas> : evict_select_kernel<false, kCtas>;
+    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(select), (int)(sizeof(SelectShared) + (size_t)kHeldKeys * 4));
+    if (e != cudaSuccess) return e;
+    return launch_pdl_cluster(kCtas, select, dim3((unsigned)(a.Hkv * kCtas)), dim3(kSelectThreads), sizeof(SelectShared) + (held ? (size_t)per * 4 : 0), s, a);
+}
+
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s) {
     const int64_t m = a.rows - a.n_sink - a.n_recent;
-    // CTAs of a cluster: one per 4096 candidates, eight at most (the portable size)
-    int ctas = 1;
-    while (ctas < 8 && (int64_t)ctas * 4096 < m) ctas *= 2;
-    const int64_t per = (m + ctas - 1) / ctas;
-    const bool held = per <= kHeldKeys;
-    auto select = held ? evict_select_kernel<true> : evict_select_kernel<false>;
-    const size_t most = sizeof(SelectShared) + (size_t)kHeldKeys * 4;
     static_assert(sizeof(SelectShared) + (size_t)kHeldKeys * 4 <= 232448, "shared memory budget of one CTA");
-    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(select), (int)most);
-    if (e != cudaSuccess) return e;
-    const size_t smem = sizeof(SelectShared) + (held ? (size_t)per * 4 : 0);
-    e = launch_pdl_cluster(ctas, select, dim3((unsigned)(a.Hkv * ctas)), dim3(kSelectThreads), smem, s, a, ctas);
+    cudaError_t e = m <= kOneCta                                        ? launch_select<1>(a, s)
+                    : m > kEightCtas && select_clusters<16>() >= a.Hkv ? launch_select<16>(a, s)
+                                                                        : launch_select<8>(a, s);
     if (e != cudaSuccess) return e;
     int lg = 0;                                      // (rows are 64 to 512 bytes, a power of two)
     while (16 << lg < a.from.row_bytes) ++lg;
