@@ -7,12 +7,12 @@
 //
 // Select.  A weight is mapped to a 32-bit key that sorts as the weight does (NaN below everything, -0 as +0).  The want-th largest key is
 // found by radix, eight bits at a time from the top: a histogram of the keys that agree with what is known so far, until all that are
-// left in the bin are wanted.  A cluster of CTAs has one KV head: each takes an equal range of rows, holds its keys in shared memory
-// (51 200 of them; a longer range is read from global memory for each histogram), and adds up the histograms of all through
-// distributed shared memory.  Then rows above the key, and as many of those equal to it as are wanted, from the lowest up, are counted
-// thread by thread (a piece of the range each, of an odd length, so that 32 of them lie in different banks), and written in
-// order.  Counts are whole numbers, so that the order of the atomics changes nothing.
-// What bounds it is latency: a sweep of shared memory, a cluster barrier (1500 cycles), a look at eight histograms and a scan for every
+// left in the bin are wanted.  A cluster of eight CTAs has one KV head (a CTA on its own, up to 4096 candidates): each takes an equal
+// range of rows and each thread a piece of it, whose keys it keeps in registers (17 at most; in shared memory up to 51 200 of a
+// CTA, else the weights are read again for each histogram); the histograms of all are added up through distributed shared memory.
+// Then rows above the key, and as many of those equal to it as are wanted, from the lowest up, are counted thread by
+// thread and written in order.  Counts are whole numbers, so that the order of the atomics changes nothing.
+// What bounds it is latency: a sweep of the keys, a cluster barrier (1500 cycles), a look at eight histograms (1000) and a scan for every
 // eight bits.  (Three histograms over 11, 11 and 10 bits: 64 KB from the peers at ~20 bytes a cycle each; numbering by ballots and
 // the weights written here took half of the 26 us.)
 //
@@ -24,16 +24,18 @@
 namespace kvf {
 namespace {
 
-constexpr int kSelectThreads = 1024;
 constexpr int kBins = 256, kPasses = 4;
+constexpr int kWide = 1024, kNarrow = 512;           // threads of a CTA of a cluster, of one on its own
+constexpr int kOwn = 17;                             // keys that a thread keeps in registers, odd
 constexpr int kHeldKeys = 51200;                     // keys of a CTA's range in shared memory
-constexpr int64_t kOneCta = 4096;                    // candidates up to which a KV head gets one CTA, not eight
+constexpr int64_t kOneCta = 8 * kNarrow;             // candidates up to which a KV head gets one CTA, not eight
 
 struct SelectShared {
     uint32_t hist[kPasses][kBins];
-    uint32_t scan[kSelectThreads / 32];
+    uint32_t scan[32];
     uint32_t found_bin, found_above, found_count;    // bin that the wanted key lies in, keys in the bins above it, in it
-    __align__(8) uint32_t counts[2];                 // of this CTA's range: keys above the wanted key, keys equal to it
+    uint32_t counts[2];                              // of this CTA's range: keys above the wanted key, keys equal to it
+    uint32_t before[2];                              // of the ranges before it
 };
 
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -49,6 +51,7 @@ __device__ __forceinline__ uint32_t peer_u32(const uint32_t *p, uint32_t rank) {
     return v;
 }
 // Sum of x over the threads up to mine; `total` of all.  Two barriers; scan[32].
+template <int kThreads>
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *scan, uint32_t &total) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
@@ -58,27 +61,24 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *scan, uint3
     }
     if (lane == 31) scan[warp] = x;
     __syncthreads();
-    uint32_t below = lane < warp ? scan[lane] : 0u, all = scan[lane];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        below += __shfl_xor_sync(0xffffffffu, below, o);
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-    }
-    total = all;
+    const uint32_t w = lane < kThreads / 32 ? scan[lane] : 0u;
+    total = __reduce_add_sync(0xffffffffu, w);
+    x += __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u);
     __syncthreads();
-    return x + below;
+    return x;
 }
 
-// kCtas: CTAs of a cluster.  kHeld: the range's keys stay in shared memory.
-template <bool kHeld, int kCtas>
-__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const EvictArgs a) {
+// kCtas: CTAs of a cluster.  kKeys: where a CTA's keys are: 0 its threads' registers, 1 shared memory, 2 nowhere (the weights are read again).
+template <int kKeys, int kCtas>
+__global__ void __launch_bounds__(kCtas > 1 ? kWide : kNarrow, 1) evict_select_kernel(const EvictArgs a) {
+    constexpr int kThreads = kCtas > 1 ? kWide : kNarrow;
     auto meet = [&]() {
         if constexpr (kCtas > 1) cluster_sync_all();
     };
     extern __shared__ __align__(16) uint8_t smem_raw[];
     SelectShared &sh = *reinterpret_cast<SelectShared *>(smem_raw);
     uint32_t *held = reinterpret_cast<uint32_t *>(smem_raw + sizeof(SelectShared));
-    const int tid = threadIdx.x, warp = tid >> 5;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = kCtas > 1 ? cluster_cta_rank() : 0u;
     const int g = blockIdx.x / kCtas;
     const float *mass = a.mass + (int64_t)g * a.mass_stride;
@@ -89,16 +89,45 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
     const int mine = (int)(min(at0 + per, m) - at0);
     const float *w0 = mass + a.n_sink + at0;
 
-    for (int i = tid; i < kPasses * kBins; i += kSelectThreads) (&sh.hist[0][0])[i] = 0u;
+    for (int i = tid; i < kPasses * kBins; i += kThreads) (&sh.hist[0][0])[i] = 0u;
     pdl_launch_dependents();
     __syncthreads();
     pdl_wait();                                                          // the weights are an earlier kernel's
+    // Keys into shared memory in the order of the rows, a thread's piece out of it again.  (Sixteen loads in flight a thread; pieces of an
+    // odd length, so that those of a warp's threads lie in different banks.)
+    const int seg = ((mine + kThreads - 1) / kThreads) | 1, s0 = min(tid * seg, mine), s1 = min(s0 + seg, mine);
+    uint32_t own[kKeys == 0 ? kOwn : 1];
+    if constexpr (kKeys < 2) {
+        for (int i = tid; i < mine; i += 16 * kThreads) {
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = i + e * kThreads < mine ? w0[i + e * kThreads] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (i + e * kThreads < mine) held[i + e * kThreads] = key_of(x[e]);
+        }
+        __syncthreads();
+    }
+    if constexpr (kKeys == 0) {
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) own[e] = s0 + e < s1 ? held[s0 + e] : 0u;
+    }
     // rows that stay whatever their weight
-    for (int64_t i = (int64_t)rank * kSelectThreads + tid; i < a.n_sink + a.n_recent; i += kCtas * kSelectThreads) {
+    for (int64_t i = (int64_t)rank * kThreads + tid; i < a.n_sink + a.n_recent; i += kCtas * kThreads) {
         const int64_t row = i < a.n_sink ? i : a.rows - a.n_recent + (i - a.n_sink);
         kept[i < a.n_sink ? i : a.budget - a.n_recent + (i - a.n_sink)] = (int32_t)row;
     }
-    auto key_at = [&](int i) { return kHeld ? held[i] : key_of(w0[i]); };
+    // f(key, its place in the range) for each of my keys, in order
+    auto each = [&](auto f) {
+        if constexpr (kKeys == 0) {
+#pragma unroll
+            for (int e = 0; e < kOwn; ++e)
+                if (s0 + e < s1) f(own[e], s0 + e);
+        } else {
+#pragma unroll 4
+            for (int i = s0; i < s1; ++i) f(kKeys == 1 ? held[i] : key_of(w0[i]), i);
+        }
+    };
 
     uint32_t known = 0u;                 // the wanted key's upper bits, as far as they are known
     uint32_t left = (uint32_t)want;      // the wanted key is the left-th largest of the keys that agree with them
@@ -107,27 +136,9 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
     for (int pass = 0; pass < kPasses && want > 0; ++pass) {
         uint32_t *hist = sh.hist[pass];
         const int shift = 24 - 8 * pass;
-        if (pass == 0) {
-            // (sixteen loads in flight a thread)
-            for (int i = tid; i < mine; i += 16 * kSelectThreads) {
-                float x[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = i + e * kSelectThreads < mine ? w0[i + e * kSelectThreads] : 0.f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (i + e * kSelectThreads >= mine) break;
-                    const uint32_t k = key_of(x[e]);
-                    if (kHeld) held[i + e * kSelectThreads] = k;
-                    atomicAdd(&hist[k >> 24], 1u);
-                }
-            }
-        } else {
-#pragma unroll 4
-            for (int i = tid; i < mine; i += kSelectThreads) {
-                const uint32_t k = key_at(i);
-                if (k >> (shift + 8) == known) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-            }
-        }
+        each([&](uint32_t k, int) {
+            if (pass == 0 || k >> (shift + 8) == known) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        });
         __syncthreads();
         meet();                          // everybody's histogram is complete (and stays: the next pass has another)
         // bins from the top down, one a thread
@@ -145,7 +156,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
             }
         }
         uint32_t all;
-        const uint32_t upto = block_scan(c, sh.scan, all);
+        const uint32_t upto = block_scan<kThreads>(c, sh.scan, all);
         if (bin >= 0 && left > upto - c && left <= upto) {
             sh.found_bin = (uint32_t)bin;
             sh.found_above = upto - c;
@@ -159,18 +170,15 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
     }
     // Wanted are the keys whose upper bits are above `known`, and of those that have them `left`, from the lowest row up.
     const int lower = 32 - bits;
-    auto above = [&](uint32_t k) { return bits > 0 && k >> lower > known; };
-    auto equal = [&](uint32_t k) { return bits > 0 && k >> lower == known; };
-    const int seg = ((mine + kSelectThreads - 1) / kSelectThreads) | 1, s0 = min(tid * seg, mine), s1 = min(s0 + seg, mine);
     uint32_t gt = 0u, eq = 0u;
-#pragma unroll 4
-    for (int i = s0; i < s1; ++i) {
-        const uint32_t k = key_at(i);
-        gt += above(k);
-        eq += equal(k);
-    }
+    if (want > 0)
+        each([&](uint32_t k, int) {
+            gt += k >> lower > known;
+            eq += k >> lower == known;
+        });
     uint32_t gt_all, eq_all;
-    uint32_t gt0 = block_scan(gt, sh.scan, gt_all) - gt, eq0 = block_scan(eq, sh.scan, eq_all) - eq;      // of rows below my piece
+    uint32_t gt0 = block_scan<kThreads>(gt, sh.scan, gt_all) - gt, eq0 = block_scan<kThreads>(eq, sh.scan, eq_all) - eq;      // of rows below my piece
+    uint32_t gt_before = 0u, eq_before = 0u;         // of the ranges before mine
     if constexpr (kCtas > 1) {
         if (tid == 0) {
             sh.counts[0] = gt_all;
@@ -178,26 +186,50 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const E
         }
         __syncthreads();
         meet();
-        uint32_t got[2 * kCtas];
-#pragma unroll
-        for (int r = 0; r < 2 * kCtas; ++r) got[r] = peer_u32(&sh.counts[r & 1], (uint32_t)(r >> 1));
-#pragma unroll
-        for (int r = 0; r < kCtas; ++r)
-            if (r < (int)rank) {
-                gt0 += got[2 * r];
-                eq0 += got[2 * r + 1];
+        if (warp == 0) {
+            uint32_t x = 0u, y = 0u;
+            if (lane < (int)rank) {
+                x = peer_u32(&sh.counts[0], (uint32_t)lane);
+                y = peer_u32(&sh.counts[1], (uint32_t)lane);
             }
+            x = __reduce_add_sync(0xffffffffu, x);
+            y = __reduce_add_sync(0xffffffffu, y);
+            if (lane == 0) {
+                sh.before[0] = x;
+                sh.before[1] = y;
+            }
+        }
+        __syncthreads();
+        gt_before = sh.before[0];
+        eq_before = sh.before[1];
+        gt0 += gt_before;
+        eq0 += eq_before;
+        cluster_arrive_relaxed();        // (my looks at the partners are over; see the end)
     }
-#pragma unroll 4
-    for (int i = s0; i < s1; ++i) {
-        const uint32_t k = key_at(i);
-        const bool over = above(k), tie = equal(k);
-        if (over || (tie && eq0 < left)) kept[a.n_sink + gt0 + min(eq0, left)] = (int32_t)(a.n_sink + at0 + i);
-        gt0 += over;
-        eq0 += tie;
+    // Numbers of the rows kept: through shared memory where the keys are no longer there, so that neighbours are written together (as they
+    // come, 5400 cycles for 16 384 keys)
+    const uint32_t first = gt_before + min(eq_before, left);             // kept rows of the ranges before mine
+    if (want > 0)
+        each([&](uint32_t k, int i) {
+            const bool over = k >> lower > known, tie = k >> lower == known;
+            if (over || (tie && eq0 < left)) {
+                const uint32_t to = gt0 + min(eq0, left);
+                const int32_t row = (int32_t)(a.n_sink + at0 + i);
+                if (kKeys == 0) held[to - first] = (uint32_t)row;
+                else kept[a.n_sink + to] = row;
+            }
+            gt0 += over;
+            eq0 += tie;
+        });
+    if constexpr (kKeys == 0) {
+        __syncthreads();
+        const int count = want > 0 ? (int)(gt_all + min(eq_before + eq_all, left) - min(eq_before, left)) : 0;
+        for (int i = tid; i < count; i += kThreads) kept[a.n_sink + first + i] = (int32_t)held[i];
     }
-    __syncthreads();
-    meet();                              // nobody leaves while a partner may still read its counts
+    if constexpr (kCtas > 1) {
+        __syncwarp();
+        cluster_wait();                  // nobody leaves while a partner may still read its counts
+    }
 }
 
 constexpr int kMoveThreads = 256, kMoveItems = 8;
@@ -252,20 +284,23 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
 
 }  // namespace
 
-template <int kCtas>
-static cudaError_t launch_select(const EvictArgs &a, cudaStream_t s) {
-    const int64_t m = a.rows - a.n_sink - a.n_recent, per = (m + kCtas - 1) / kCtas;
-    const bool held = per <= kHeldKeys;
-    auto select = held ? evict_select_kernel<true, kCtas> : evict_select_kernel<false, kCtas>;
-    cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(select), (int)(sizeof(SelectShared) + (size_t)kHeldKeys * 4));
+template <int kKeys, int kCtas>
+static cudaError_t launch_select(const EvictArgs &a, int64_t per, cudaStream_t s) {
+    auto select = evict_select_kernel<kKeys, kCtas>;
+    const cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(select), (int)(sizeof(SelectShared) + (size_t)kHeldKeys * 4));
     if (e != cudaSuccess) return e;
-    return launch_pdl_cluster(kCtas, select, dim3((unsigned)(a.Hkv * kCtas)), dim3(kSelectThreads), sizeof(SelectShared) + (held ? (size_t)per * 4 : 0), s, a);
+    return launch_pdl_cluster(kCtas, select, dim3((unsigned)(a.Hkv * kCtas)), dim3(kCtas > 1 ? kWide : kNarrow),
+                              sizeof(SelectShared) + (kKeys < 2 ? (size_t)per * 4 : 0), s, a);
 }
 
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s) {
-    const int64_t m = a.rows - a.n_sink - a.n_recent;
+    const int64_t m = a.rows - a.n_sink - a.n_recent, per = (m + 7) / 8;
     static_assert(sizeof(SelectShared) + (size_t)kHeldKeys * 4 <= 232448, "shared memory budget of one CTA");
-    cudaError_t e = m <= kOneCta ? launch_select<1>(a, s) : launch_select<8>(a, s);
+    static_assert(kOneCta <= kOwn * kNarrow, "a thread's keys");
+    cudaError_t e = m <= kOneCta        ? launch_select<0, 1>(a, m, s)
+                    : per <= 16 * kWide ? launch_select<0, 8>(a, per, s)
+                    : per <= kHeldKeys  ? launch_select<1, 8>(a, per, s)
+                                        : launch_select<2, 8>(a, per, s);
     if (e != cudaSuccess) return e;
     int lg = 0;                                      // (rows are 64 to 512 bytes, a power of two)
     while (16 << lg < a.from.row_bytes) ++lg;
