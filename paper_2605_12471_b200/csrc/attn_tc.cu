@@ -96,6 +96,7 @@
 namespace kvf {
 namespace {
 
+enum { kPlain = 0, kRanged, kCapped, kBiased };
 constexpr int kRows = 128;                    // rows of a Q tile = keys of a K/V tile
 constexpr int kD = 128;                       // head_dim
 constexpr uint32_t kPanel = 128 * 128;        // bytes of a [128 rows][64 bf16] swizzled panel
@@ -208,15 +209,17 @@ __device__ __forceinline__ void exp_half_small(const ScoreMods &m, const uint32_
 // when every row pair has two row tiles (a chunk of a multiple of 512 / G tokens).
 // kEarly (bf16 rows, chunks of two row tiles): Q K^T of the next key tile is issued under the softmax of the
 // current one, see the issuer.
-// kScored (bf16 rows, no window): capped or biased scores, a range of rows per token (ScoreMods).  Scores are brought to log2 units
-// before the softmax.  With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the
-// line of all tiles is.
+// kMods (bf16 rows, no window): what a scored step does to its scores (ScoreMods).  kRanged: a range of rows per token, nothing else;
+// kCapped: a cap as well; kBiased: a bias, and a cap or none.  Capped and biased scores are brought to log2 units before the softmax.
+// With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the line of all tiles is.
+// 256 tokens of 32 / 8 heads at prefix 31 K: plain 108 us, capped 139 (scores up to half the cap), biased XXX.
 // kRanks (bf16 rows, two streams): a cluster of that many CTAs has one row tile of one KV head, each an equal share of its key
 // tiles, and writes the output: no partial results, no merge kernel.  See the end of the kernel.
-template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0, bool kScored = false>
+template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0, int kMods = kPlain>
 __global__ void __launch_bounds__(kQuant ? kThreadsQ8 : kThreads, 1)
 attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v) {
+    constexpr bool kScored = kMods != kPlain;
     static_assert(!kEarly || kQuant == 0 || kPair, "the early issue needs the space of a K/V slot for its probabilities");
     constexpr int NS = kQuant ? kSlotsQ8 : kEarly ? kSlotsEarly : kSlots;        // slots behind the Q tiles: the shared ring's
     constexpr int SR = kQuant ? 2 : 3;                     // slots of each stream's own ring
@@ -733,7 +736,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
             clear = (int64_t)__reduce_min_sync(0xffffffffu, (int)min(limit_s, (int64_t)INT_MAX));
             clear_from = (int64_t)__reduce_max_sync(0xffffffffu, (int)begin_s);
         }
-        const float sl2 = kScored ? 1.f : a.scale_log2;          // (kScored: scores come in log2 units)
+        const float sl2 = kMods >= kCapped ? 1.f : a.scale_log2;          // (capped or biased: scores come in log2 units)
         const float2 sl2v = make_float2(sl2, sl2);
         const int64_t nG = (int64_t)nmax * G;                 // rows of a partial slot
 
@@ -800,9 +803,9 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
             }
             float m_ref = -INFINITY;   // reference maximum (raw score units) the probabilities are scaled by
             float l = 0.f;
-            // (kScored) the head's slope in log2 units per row of distance
+            // (kBiased) the head's slope in log2 units per row of distance
             float slope = 0.f;
-            if (kScored && a.mods.slopes && valid) slope = a.mods.slopes[kvh * a.G + gi] * kLog2e;
+            if (kMods == kBiased && valid) slope = a.mods.slopes[kvh * a.G + gi] * kLog2e;
             for (int j = j0, k = 0; j < ntiles; j += jstep, ++it, ++k) {
                 ok = mbar_wait(bar(B_SFULL0 + i), it & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
@@ -833,12 +836,13 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 KVF_TMEM_LD32(sc, 64, t_s + 64);
                 KVF_TMEM_LD32(sc, 96, t_s + 96);
                 tmem_wait_ld();
-                bool in_place = true;          // (kScored) the scores in sc are what the softmax takes; else small[] is yet to come
+                bool in_place = true;          // (kCapped) the scores in sc are what the softmax takes; else small[] is yet to come
                 float m_small = 0.f;
-                if constexpr (kScored) {
+                if constexpr (kMods >= kCapped) {
                     auto pair = [&](int c) { return make_float2(__uint_as_float(sc[c]), __uint_as_float(sc[c + 1])); };
                     auto put = [&](int c, float2 x) { sc[c] = __float_as_uint(x.x); sc[c + 1] = __float_as_uint(x.y); };
-                    if (a.mods.cap_out > 0.f) {
+                    const bool cap = kMods == kCapped || a.mods.cap_out > 0.f;
+                    if (cap) {
                         // what the tile's largest score in magnitude allows (rows past the chunk's end do not count)
                         float hi[4], lo[4];
 #pragma unroll
@@ -856,7 +860,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                         const float top = fmaxf(max3(hi[0], hi[1], hi[2]), hi[3]), low = fminf(min3(lo[0], lo[1], lo[2]), lo[3]);
                         const float far = valid ? fmaxf(top, -low) : 0.f;
                         if (!__any_sync(0xffffffffu, far > a.mods.small_to)) {
-                            if (!masked && !a.mods.slopes) {
+                            if (kMods == kCapped && !masked) {
                                 in_place = false;
                                 m_small = top * cap_small_over(a.mods, both(top)).x;
                             } else {
@@ -870,34 +874,41 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
 #pragma unroll
                             for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(cap_any(a.mods, __uint_as_float(sc[c])));
                         }
-                    } else {
-                        const float2 by = both(a.scale_log2);
-#pragma unroll
-                        for (int c = 0; c < 128; c += 2) put(c, __fmul2_rn(pair(c), by));
                     }
-                    if (a.mods.slopes) {
+                    if constexpr (kMods == kBiased) {
                         const int64_t behind = a.mods.pos0 + tok - key0;          // distance of the tile's first key
                         const float at = (float)behind;
+                        const float2 by = both(cap ? 1.f : a.scale_log2);
                         if (__all_sync(0xffffffffu, !valid || behind >= kRows - 1)) {
                             const float2 from = both(-slope * at), per = both(slope);
 #pragma unroll
-                            for (int c = 0; c < 128; c += 2) put(c, __fadd2_rn(pair(c), __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from)));
+                            for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), by, __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from)));
                         } else {
 #pragma unroll
-                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(fmaf(-slope, fabsf(at - (float)c), __uint_as_float(sc[c])));
+                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(fmaf(__uint_as_float(sc[c]), by.x, -slope * fabsf(at - (float)c)));
                         }
                     }
                 }
+                if constexpr (kScored) {
+                    // a row sees [begin_s, limit_s): what lies before it and behind it, if a row of the warp has any
+                    const int from = (int)max((int64_t)0, min((int64_t)kRows, begin_s - key0));
+                    if (masked && __any_sync(0xffffffffu, nvis < kRows))
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) sc[c] = c < nvis ? sc[c] : 0xFF800000u;
+                    if (masked && __any_sync(0xffffffffu, from > 0))
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) sc[c] = c >= from ? sc[c] : 0xFF800000u;
+                } else
                 if (masked) {
                     // columns below lo_c lie before the window and count only if they are sinks
                     const int lo_c = kWindow ? (int)max((int64_t)0, min((int64_t)kRows, a.win_lo - key0))
-                                   : kScored ? (int)max((int64_t)0, min((int64_t)kRows, begin_s - key0)) : 0;
+                                   : 0;
                     const int sink_c = kWindow ? (int)max((int64_t)0, min((int64_t)kRows, a.n_sink - key0)) : 0;
 #pragma unroll
                     for (int c = 0; c < 128; ++c) sc[c] = (c < nvis && (c >= lo_c || c < sink_c)) ? sc[c] : 0xFF800000u;   // -inf
                 }
                 float m_tile = m_small;
-                if (!kScored || in_place) {
+                if (kMods != kCapped || in_place) {
                 float mx[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) mx[q] = fmaxf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
@@ -954,7 +965,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
 
                 // probabilities; the first 64 keys are handed over before the rest is computed
                 uint32_t p[32];
-                if (kScored && !in_place) exp_half_small(a.mods, sc, p, negv, acc0, acc1);
+                if (kMods == kCapped && !in_place) exp_half_small(a.mods, sc, p, negv, acc0, acc1);
                 else exp_half(sc, p, sl2v, negv, acc0, acc1);
                 KVF_TMEM_ST32(p, 0, t_s);
                 tmem_wait_st();
@@ -965,7 +976,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 // takes ~250 cycles to come even if it is yes; every phase is waited for)
                 uint32_t panel_free = 1;
                 if (kEarly && k > 0) panel_free = mbar_test(bar(B_PVDONE0 + i), (it - 1) & 1);
-                if (kScored && !in_place) exp_half_small(a.mods, sc + 64, p, negv, acc0, acc1);
+                if (kMods == kCapped && !in_place) exp_half_small(a.mods, sc + 64, p, negv, acc0, acc1);
                 else exp_half(sc + 64, p, sl2v, negv, acc0, acc1);
                 if (kEarly) {
                     if (!__all_sync(0xffffffffu, panel_free)) ok = wait_pv();
@@ -1574,7 +1585,9 @@ cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     const bool quant = a.quant_bits != 0;
     auto kernel = a.quant_bits == 8 ? (a.win_lo > 0 ? attn_tc_kernel<true, 8, false, false> : attn_tc_kernel<false, 8, false, false>)
                 : a.quant_bits == 4 ? (a.win_lo > 0 ? attn_tc_kernel<true, 4, false, false> : attn_tc_kernel<false, 4, false, false>)
-                : a.scored          ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, true> : attn_tc_kernel<false, 0, false, false, 0, true>)
+                : a.scored && a.mods.slopes      ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kBiased> : attn_tc_kernel<false, 0, false, false, 0, kBiased>)
+                : a.scored && a.mods.cap_out > 0 ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kCapped> : attn_tc_kernel<false, 0, false, false, 0, kCapped>)
+                : a.scored                       ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kRanged> : attn_tc_kernel<false, 0, false, false, 0, kRanged>)
                                     : a.streams == 1      ? (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, true> : attn_tc_kernel<false, 0, false, true>)
                                     : (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, false> : attn_tc_kernel<false, 0, false, false>);
     const uint32_t smem = quant ? kSmemBytesQ8 : kSmemBytes;
