@@ -842,6 +842,13 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     auto pair = [&](int c) { return make_float2(__uint_as_float(sc[c]), __uint_as_float(sc[c + 1])); };
                     auto put = [&](int c, float2 x) { sc[c] = __float_as_uint(x.x); sc[c + 1] = __float_as_uint(x.y); };
                     const bool cap = kMods == kCapped || a.mods.cap_out > 0.f;
+                    // (kBiased) distance of the tile's first key; all of the tile's keys behind the token: the bias is a line
+                    const int64_t behind = kMods == kBiased ? a.mods.pos0 + tok - key0 : 0;
+                    const float at = (float)behind;
+                    const bool line = kMods == kBiased && __all_sync(0xffffffffu, !valid || behind >= kRows - 1);
+                    const float2 from = both(-slope * at), per = both(slope);
+                    auto on_line = [&](int c) { return __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from); };
+                    bool biased = false;
                     if (cap) {
                         // what the tile's largest score in magnitude allows (rows past the chunk's end do not count)
                         float hi[4], lo[4];
@@ -863,6 +870,10 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                             if (kMods == kCapped && !masked) {
                                 in_place = false;
                                 m_small = top * cap_small_over(a.mods, both(top)).x;
+                            } else if (kMods == kBiased && line) {
+                                biased = true;
+#pragma unroll
+                                for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), cap_small_over(a.mods, pair(c)), on_line(c)));
                             } else {
 #pragma unroll
                                 for (int c = 0; c < 128; c += 2) put(c, __fmul2_rn(pair(c), cap_small_over(a.mods, pair(c))));
@@ -876,13 +887,12 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                         }
                     }
                     if constexpr (kMods == kBiased) {
-                        const int64_t behind = a.mods.pos0 + tok - key0;          // distance of the tile's first key
-                        const float at = (float)behind;
                         const float2 by = both(cap ? 1.f : a.scale_log2);
-                        if (__all_sync(0xffffffffu, !valid || behind >= kRows - 1)) {
-                            const float2 from = both(-slope * at), per = both(slope);
+                        if (biased) {
+                            // (with the cap)
+                        } else if (line) {
 #pragma unroll
-                            for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), by, __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from)));
+                            for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), by, on_line(c)));
                         } else {
 #pragma unroll
                             for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(fmaf(__uint_as_float(sc[c]), by.x, -slope * fabsf(at - (float)c)));
