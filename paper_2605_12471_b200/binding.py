@@ -215,6 +215,9 @@ def _scores(softcap, slopes, first, end, heads: int, n: int) -> Optional[kvf_sco
 class Cache:
     """One layer's accumulated K/V on the current CUDA device (kvf_cache_* calls)."""
 
+    _k_view: Optional[torch.Tensor] = None      # the planes' views, made when first asked for
+    _v_view: Optional[torch.Tensor] = None
+
     def __init__(self, cfg: kvf_config, device: str | torch.device = "cuda", workspace: torch.Tensor | None = None):
         lib = load()
         self.cfg = cfg
@@ -438,10 +441,14 @@ class Cache:
 
     def k_plane(self) -> torch.Tensor:
         """[Hkv, capacity, d] view of the rotated keys (rows >= len are not content)."""
-        return self._plane(load().kvf_cache_k_plane(self._h))
+        if self._k_view is None or self.cfg.flags & KVF_CACHE_INT4:      # (int4: a copy, made each time)
+            self._k_view = self._plane(load().kvf_cache_k_plane(self._h))
+        return self._k_view
 
     def v_plane(self) -> torch.Tensor:
-        return self._plane(load().kvf_cache_v_plane(self._h))
+        if self._v_view is None or self.cfg.flags & KVF_CACHE_INT4:
+            self._v_view = self._plane(load().kvf_cache_v_plane(self._h))
+        return self._v_view
 
     def plan(self, n_tokens: int, prefix_len: Optional[int] = None) -> Tuple[int, int, int, int]:
         arr = (ctypes.c_int32 * 4)()

@@ -60,6 +60,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a
     const T *Kp = reinterpret_cast<const T *>(a.k_plane) + (int64_t)kvh * a.capacity * D;
     const T *Vp = reinterpret_cast<const T *>(a.v_plane) + (int64_t)kvh * a.capacity * D;
 
+    if (kScored) {
+        pdl_launch_dependents();
+        pdl_wait();                      // (launched dependently; the rotated chunk is read from here on)
+    }
     // key-tile range of this split; the row tile needs keys below P + (last token + 1)
     const int row0 = tile * BM;
     const int tok_last = min(n - 1, (row0 + BM - 1) / G);
@@ -272,6 +276,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_simt_kernel(const AttnArgs a
 template <int D>
 __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a) {
     const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;   // (row, float4 column)
+    pdl_launch_dependents();
+    pdl_wait();                          // (behind a scored step's attention it is launched dependently)
     const int64_t rows = (int64_t)a.n * a.H;
     if (idx >= rows * (D / 4)) return;
     const int64_t row = idx / (D / 4);
@@ -310,6 +316,7 @@ cudaError_t launch_simt_k(const AttnArgs &a, cudaStream_t s, int *grid_out) {
     if (e != cudaSuccess) return e;
     dim3 grid((a.n * a.G + BM - 1) / BM, a.Hkv, a.splits);
     if (grid_out) *grid_out = grid.x * grid.y * grid.z;
+    if (kScored) return launch_pdl(attn_simt_kernel<T, D, kScored>, grid, dim3(kThreads), smem, s, a);
     attn_simt_kernel<T, D, kScored><<<grid, kThreads, smem, s>>>(a);
     return cudaGetLastError();
 }
@@ -338,6 +345,7 @@ cudaError_t launch_combine(const AttnArgs &a, int dtype, cudaStream_t s) {
     (void)dtype;
     int64_t items = (int64_t)a.n * a.H * (a.d / 4);
     int blocks = (int)((items + 255) / 256);
+    if (a.scored) return launch_pdl(a.d == 128 ? combine_kernel<128> : combine_kernel<64>, dim3(blocks), dim3(256), 0, s, a);
     if (a.d == 128) combine_kernel<128><<<blocks, 256, 0, s>>>(a);
     else if (a.d == 64) combine_kernel<64><<<blocks, 256, 0, s>>>(a);
     else return cudaErrorInvalidValue;

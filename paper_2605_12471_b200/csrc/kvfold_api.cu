@@ -490,7 +490,8 @@ Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t
         // one wave: as many splits as still fit the machine at once (a second, partly filled
         // wave would double the time), but keep at least 4 key tiles per split
         int want = target / units;
-        int64_t cap = nt / 4;
+        // (scored steps have no one-launch form to fall back on for few tiles: one a split then, 64 tokens of 4 / 1 heads at 448: 39 -> 19 us)
+        int64_t cap = scored ? nt : nt / 4;
         if (want > cap) want = (int)cap;
         splits = want;
     }
