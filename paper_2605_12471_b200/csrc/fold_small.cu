@@ -21,6 +21,7 @@
 // 0.34, half of the stall cycles on them), so slices are as short as the device has room for.  Tried: 4 x 4 blocks
 // per thread on half the threads (a third less shared-memory traffic, fewer warps: 6.3 us a tile).
 #include "kvfold_internal.h"
+#include "scores.cuh"
 #include "sm100_ptx.cuh"
 
 namespace kvf {
@@ -106,8 +107,8 @@ __device__ __forceinline__ void to_shared(float *dst, const float (&x)[N]) {
     for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(dst + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
 }
 
-// BN = keys of a tile: 64, or 32 (see fold_small_cut).
-template <typename T, bool INTERLEAVED, int BN>
+// BN = keys of a tile: 64, or 32 (see fold_small_cut).  kScored: scores capped, biased and masked by a range of rows per token (ScoreMods).
+template <typename T, bool INTERLEAVED, int BN, bool kScored>
 __global__ void __launch_bounds__(kThreads, 2) fold_small_kernel(const __grid_constant__ RopeAppendArgs r, const __grid_constant__ AttnArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T);
     constexpr int RC = HALF / VEC;                       // vectors of half a row
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 2) fold_small_kernel(const __grid_co
     // this row tile sees the keys below `need`; its key tiles are cut into equal slices
     const int row0 = tile * BM;
     const int tok0 = row0 / G, tok_last = min(n - 1, (row0 + BM - 1) / G);
-    const int64_t need = P + (tok_last + 1) * a.self_rows;
+    const int64_t need = P + (kScored && a.mods.end ? n : tok_last + 1) * a.self_rows;
     const WindowTiles wt(a.win_lo, a.n_sink, BN);
     const int nt = (int)((need + BN - 1) / BN) - wt.skip;
     const int kt_begin = (int)((int64_t)rank * nt / ranks), kt_end = (int)((int64_t)(rank + 1) * nt / ranks);
@@ -215,10 +216,18 @@ __global__ void __launch_bounds__(kThreads, 2) fold_small_kernel(const __grid_co
     }
 
     int64_t limit[TR];    // keys below limit are visible to row TR * ty + i
+    int64_t begin[kScored ? TR : 1];
+    float slope[kScored ? TR : 1];
 #pragma unroll
     for (int i = 0; i < TR; ++i) {
         const int tok = (row0 + TR * ty + i) / G;
         limit[i] = tok < n ? P + (tok + 1) * a.self_rows : 0;
+        if constexpr (kScored) {
+            const RowRange seen = tok < n ? seen_rows(a.mods, tok, tok, P, P + n * a.self_rows, a.self_rows) : RowRange{0, 0};
+            begin[i] = seen.begin;
+            limit[i] = seen.end;
+            slope[i] = a.mods.slopes && tok < n ? a.mods.slopes[kvh * G + (row0 + TR * ty + i) % G] * kLog2e : 0.f;
+        }
     }
     float m[TR], l[TR];
     float2 acc[TR][2] = {};
@@ -292,8 +301,18 @@ __global__ void __launch_bounds__(kThreads, 2) fold_small_kernel(const __grid_co
 #pragma unroll
             for (int j = 0; j < NK; ++j) {
                 const int64_t key = key0 + tx + 16 * j;
+                if constexpr (kScored) {
+                    const float dot = s2[i][j].x + s2[i][j].y;
+                    float x = a.mods.cap_out > 0.f ? a.mods.cap_out * tanhf(dot * a.mods.cap_in) : dot * a.scale_log2;
+                    if (a.mods.slopes) {
+                        const int64_t far = a.mods.pos0 + (row0 + TR * ty + i) / G - key;
+                        x = fmaf(-slope[i], (float)(far < 0 ? -far : far), x);
+                    }
+                    s[i][j] = key >= begin[i] && key < limit[i] ? x : -INFINITY;
+                } else {
                 const bool vis = key < limit[i] && (key >= a.win_lo || key < a.n_sink);
                 s[i][j] = vis ? (s2[i][j].x + s2[i][j].y) * a.scale_log2 : -INFINITY;
+                }
                 mx = fmaxf(mx, s[i][j]);
             }
 #pragma unroll
@@ -407,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 2) fold_small_kernel(const __grid_co
 
 // Once per kernel and device: shared-memory limit, clusters of 16 CTAs (beyond the portable eight), and how many clusters
 // of each width the device holds at once.
-template <typename T, bool INTERLEAVED, int BN>
+template <typename T, bool INTERLEAVED, int BN, bool kScored>
 cudaError_t prepare_once(FoldSmallFit *fit) {
     struct Done { int dev; FoldSmallFit fit; };
     static std::mutex mu;
@@ -421,7 +440,7 @@ cudaError_t prepare_once(FoldSmallFit *fit) {
             if (fit) *fit = d.fit;
             return cudaSuccess;
         }
-    auto kernel = fold_small_kernel<T, INTERLEAVED, BN>;
+    auto kernel = fold_small_kernel<T, INTERLEAVED, BN, kScored>;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
     if (e != cudaSuccess) return e;
     Done now = {dev, {}};
@@ -450,9 +469,9 @@ cudaError_t prepare_once(FoldSmallFit *fit) {
     return cudaSuccess;
 }
 
-template <typename T, bool INTERLEAVED, int BN>
+template <typename T, bool INTERLEAVED, int BN, bool kScored>
 cudaError_t launch_bn(const RopeAppendArgs &r, const AttnArgs &a, int ranks, cudaStream_t s) {
-    cudaError_t e = prepare_once<T, INTERLEAVED, BN>(nullptr);
+    cudaError_t e = prepare_once<T, INTERLEAVED, BN, kScored>(nullptr);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(fold_small_row_tiles(a.n, a.G), a.Hkv, ranks);
@@ -468,12 +487,13 @@ cudaError_t launch_bn(const RopeAppendArgs &r, const AttnArgs &a, int ranks, cud
     attr[1].val.clusterDim.z = (unsigned)ranks;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, fold_small_kernel<T, INTERLEAVED, BN>, r, a);
+    return cudaLaunchKernelEx(&cfg, fold_small_kernel<T, INTERLEAVED, BN, kScored>, r, a);
 }
 
 template <typename T, bool INTERLEAVED>
 cudaError_t launch_t(const RopeAppendArgs &r, const AttnArgs &a, const FoldSmallCut &cut, cudaStream_t s) {
-    return cut.keys == 32 ? launch_bn<T, INTERLEAVED, 32>(r, a, cut.ranks, s) : launch_bn<T, INTERLEAVED, 64>(r, a, cut.ranks, s);
+    if (a.scored) return cut.keys == 32 ? launch_bn<T, INTERLEAVED, 32, true>(r, a, cut.ranks, s) : launch_bn<T, INTERLEAVED, 64, true>(r, a, cut.ranks, s);
+    return cut.keys == 32 ? launch_bn<T, INTERLEAVED, 32, false>(r, a, cut.ranks, s) : launch_bn<T, INTERLEAVED, 64, false>(r, a, cut.ranks, s);
 }
 
 }  // namespace
@@ -512,9 +532,9 @@ FoldSmallCut fold_small_cut(int row_tiles, int64_t keys, bool window, const Fold
     return best;
 }
 
-// (the eight kernels differ in arithmetic and tile width only, in neither threads, shared memory nor the limit on registers: what
+// (the sixteen kernels differ in arithmetic and tile width only, in neither threads, shared memory nor the limit on registers: what
 // fits one fits all)
-cudaError_t fold_small_fit(FoldSmallFit *fit) { return prepare_once<float, false, 64>(fit); }
+cudaError_t fold_small_fit(FoldSmallFit *fit) { return prepare_once<float, false, 64, false>(fit); }
 
 cudaError_t launch_fold_small(const RopeAppendArgs &r, const AttnArgs &a, const FoldSmallCut &cut, int dtype, bool interleaved, cudaStream_t s) {
     if (a.d != D) return cudaErrorInvalidValue;

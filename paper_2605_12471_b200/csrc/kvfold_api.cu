@@ -325,14 +325,13 @@ int64_t window_lo(const kvf_cache *c, int64_t prefix) {
 }
 
 // (`ragged`: the members' row counts are known on the device only, and with them which ranges a KV head has)
-// (`scored`: capped, biased or range-masked scores - not in one launch, and fp32 rows on the CUDA cores)
+// (`scored`: capped, biased or range-masked scores - fp32 rows on the CUDA cores)
 Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t part_rows_cap = -1, bool one_launch = true, bool ragged = false,
                bool scored = false) {
     if (part_rows_cap < 0) part_rows_cap = c->part_rows_cap;
     Plan p;
     p.qdec = p.small = false;
     p.tc = c->tc || (c->tc32 && !scored);
-    one_launch = one_launch && !scored;
     p.ngroups = p.ranks = 0;
     const int64_t L = prefix + n;
     const int Hkv = c->cfg.n_kv_heads;
@@ -490,7 +489,7 @@ Plan make_plan(const kvf_cache *c, int n, int64_t prefix, int batch = 1, int64_t
         // one wave: as many splits as still fit the machine at once (a second, partly filled
         // wave would double the time), but keep at least 4 key tiles per split
         int want = target / units;
-        // (scored steps have no one-launch form to fall back on for few tiles: one a split then, 64 tokens of 4 / 1 heads at 448: 39 -> 19 us)
+        // (scored steps pay more for a tile: as few as one a split, 64 tokens of 4 / 1 heads at prefix 448 39 -> 19 us)
         int64_t cap = scored ? nt : nt / 4;
         if (want > cap) want = (int)cap;
         splits = want;
