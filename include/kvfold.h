@@ -262,8 +262,8 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  *   softcap  >= 0 and finite, 0 = none       slopes   device, [n_q_heads] fp32, or NULL
  *   first    device, [n_tokens] int32, or NULL       end      device, [n_tokens] int32, or NULL
  * The device arrays are read in stream order and may be changed behind the call.  Everything else - rows appended whatever the ranges
- * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend.  Not under a sink + window mask
- * and not on quantised storage (KVF_ERR_UNSUPPORTED).  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
+ * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend, on every storage.  Not under a sink +
+ * window mask (KVF_ERR_UNSUPPORTED).  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
  * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
  * A cap rounds each score to about 2^-20 of the largest it can become.
  */
@@ -515,6 +515,16 @@ kvf_status kvf_batch_fold_step_ragged(kvf_batch *b, const void *q, const void *k
 kvf_status kvf_batch_fold_step_varlen(kvf_batch *b, const void *q, const void *k_new, const void *v_new,
                                       const int32_t *n_tokens, int32_t max_tokens, const int64_t *pos0_or_null,
                                       void *out, float *lse_or_null, void *cuda_stream);
+
+/*
+ * The scored step (kvf_scores) for every member at once: kvf_batch_fold_step's where the members hold the same number of rows and
+ * start at the same position, else kvf_batch_fold_step_ragged's, or with n_tokens (host array) kvf_batch_fold_step_varlen's, whose
+ * layouts and conditions hold.  scores->slopes is common to the members; scores->first and scores->end are device arrays
+ * [n_caches][max_tokens], row numbers of each member's own cache.
+ */
+kvf_status kvf_batch_fold_step_scored(kvf_batch *b, const void *q, const void *k_new, const void *v_new, const int32_t *n_tokens_or_null,
+                                      int32_t max_tokens, const int64_t *pos0_or_null, const kvf_scores *scores, void *out,
+                                      float *lse_or_null, void *cuda_stream);
 
 /* kvf_cache_plan for a step of kvf_batch_fold_step; plan[2] counts the CTAs of all members.  (Steps of members that differ may be cut
  * into fewer ranges: their partial results are merged by a kernel to which many parts cost more.) */

@@ -31,7 +31,7 @@ EXPORTS = [
     "kvf_batch_status_word", "kvf_batch_launch_count", "kvf_batch_destroy", "kvf_cache_set_window",
     "kvf_batch_fold_step_ragged", "kvf_cache_k_scales", "kvf_cache_v_scales", "kvf_cache_sm_clock",
     "kvf_cache_host_flush", "kvf_batch_fold_step_varlen", "kvf_cache_flush",
-    "kvf_fold_step_scored", "kvf_attend_scored", "kvf_rotate_queries", "kvf_cache_mass", "kvf_cache_evict",
+    "kvf_fold_step_scored", "kvf_attend_scored", "kvf_batch_fold_step_scored", "kvf_rotate_queries", "kvf_cache_mass", "kvf_cache_evict",
 ]
 
 
@@ -101,6 +101,8 @@ def load() -> ctypes.CDLL:
     lib.kvf_fold_step_scored.restype = ctypes.c_int
     lib.kvf_attend_scored.argtypes = [vp, vp, i32, i64, scp, vp, vp, vp]
     lib.kvf_attend_scored.restype = ctypes.c_int
+    lib.kvf_batch_fold_step_scored.argtypes = [vp, vp, vp, vp, ctypes.POINTER(i32), i32, ctypes.POINTER(i64), scp, vp, vp, vp]
+    lib.kvf_batch_fold_step_scored.restype = ctypes.c_int
     lib.kvf_rotate_queries.argtypes = [vp, vp, i32, i64, vp, vp]
     lib.kvf_rotate_queries.restype = ctypes.c_int
     lib.kvf_cache_mass.argtypes = [vp, vp, i32, i32, i64, scp, vp, vp, i64, ctypes.c_float, vp, i64, vp]
@@ -577,10 +579,18 @@ class Batch:
 
     def fold_step(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, pos0=None,
                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-                  stream: Optional[torch.cuda.Stream] = None, ragged: bool = False) -> torch.Tensor:
+                  stream: Optional[torch.cuda.Stream] = None, ragged: bool = False, softcap: float = 0.0,
+                  slopes: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None,
+                  end: Optional[torch.Tensor] = None) -> torch.Tensor:
         """kvf_batch_fold_step, or with ragged=True kvf_batch_fold_step_ragged (members of different
-        length; pos0 is then None or one position per member)."""
+        length; pos0 is then None or one position per member).  With any of softcap, slopes ([H] fp32), first, end
+        ([n_caches, n] int32) kvf_batch_fold_step_scored."""
         assert q.dim() == 4 and q.shape[0] == len(self.caches)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1])
+        if scores is not None:
+            if pos0 is not None and not ragged:
+                pos0 = [pos0] * len(self.caches)
+            return self._fold_scored(q, k_new, v_new, None, pos0, scores, out, lse, stream)
         n = q.shape[1]
         for t in (q, k_new, v_new):
             assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16
@@ -604,11 +614,31 @@ class Batch:
             raise KvfError(rc, "kvf_batch_fold_step")
         return out
 
+    def _fold_scored(self, q, k_new, v_new, n_tokens, pos0, scores, out, lse, stream) -> torch.Tensor:
+        for t in (q, k_new, v_new):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16
+        if out is None:
+            od = torch.float32 if (self.cfg.flags & KVF_OUT_F32) else torch.bfloat16
+            out = torch.empty(q.shape, dtype=od, device=q.device)
+        ns = None if n_tokens is None else (ctypes.c_int32 * len(self.caches))(*[int(x) for x in n_tokens])
+        arr = None if pos0 is None else (ctypes.c_int64 * len(self.caches))(*[int(p) for p in pos0])
+        rc = load().kvf_batch_fold_step_scored(self._h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ns, q.shape[1], arr,
+                                               ctypes.byref(scores), out.data_ptr(), lse.data_ptr() if lse is not None else None,
+                                               _stream_ptr(stream))
+        if rc != KVF_OK:
+            raise KvfError(rc, "kvf_batch_fold_step_scored")
+        return out
+
     def fold_step_varlen(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, n_tokens, pos0=None,
                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """kvf_batch_fold_step_varlen: member i folds the first n_tokens[i] rows of its block (0 = sits out)."""
+                         stream: Optional[torch.cuda.Stream] = None, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                         first: Optional[torch.Tensor] = None, end: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """kvf_batch_fold_step_varlen: member i folds the first n_tokens[i] rows of its block (0 = sits out).  With any of
+        softcap, slopes ([H] fp32), first, end ([n_caches, longest] int32) kvf_batch_fold_step_scored."""
         assert q.dim() == 4 and q.shape[0] == len(self.caches) == len(n_tokens)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1])
+        if scores is not None:
+            return self._fold_scored(q, k_new, v_new, n_tokens, pos0, scores, out, lse, stream)
         for t in (q, k_new, v_new):
             assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16
         if out is None:

@@ -279,7 +279,7 @@ __device__ __forceinline__ void value_fragment(const uint32_t (&w)[4][BITS / 2],
     }
 }
 
-// kScored (bf16 rows): capped or biased scores, a range of rows per token (ScoreMods); the ranges' key tiles, those that a token of the
+// kScored: capped or biased scores, a range of rows per token (ScoreMods); the ranges' key tiles, those that a token of the
 // step sees, are cut among a KV head's CTAs as all of them are without.
 template <int BITS, int NB, bool kScored = false>
 __global__ void __launch_bounds__(Geo<BITS, NB>::kThreads, 1)
@@ -614,8 +614,8 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if (kScored && a.mods.cap_out > 0.f) sacc[j][nb][e] = cap_any(a.mods, sacc[j][nb][e]);
-                        else sacc[j][nb][e] *= BITS == 16 ? sl2[nb][e & 1] : row_scale[j][e >> 1] * sl2[nb][e & 1];
+                        sacc[j][nb][e] *= BITS == 16 ? sl2[nb][e & 1] : row_scale[j][e >> 1] * sl2[nb][e & 1];
+                        if (kScored && a.mods.cap_out > 0.f) sacc[j][nb][e] = cap_log2(a.mods, sacc[j][nb][e]);
                     }
             if constexpr (kScored) {
                 if (a.mods.slopes) {
@@ -624,7 +624,7 @@ attn_q8_decode_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             // distance of my first key (key g of the 64)
-                            const float at = (float)(a.mods.pos0 + (8 * nb + 2 * t4 + e) / G - key_h - g);
+                            const float at = (float)(a.mods.position(cb, (8 * nb + 2 * t4 + e) / G) - key_h - g);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 sacc[j][nb][e] = fmaf(-slope[nb][e], fabsf(at - 16.f * j), sacc[j][nb][e]);
@@ -876,7 +876,9 @@ cudaError_t launch_attn_q8_decode(const AttnArgs &a, const TcMaps &maps, cudaStr
     static_assert(Geo<16, 1>::kWarps * kMergeWarp <= Geo<16, 1>::kOffCtl, "the merge area reuses the ring");
     const bool wide = a.n * a.G > 8;
     const int bits = a.quant_bits ? a.quant_bits : 16;              // 16: plain bf16 rows
-    auto kernel = bits == 4 ? (wide ? attn_q8_decode_kernel<4, 2> : attn_q8_decode_kernel<4, 1>)
+    auto kernel = a.scored && bits < 16 ? (bits == 4 ? (wide ? attn_q8_decode_kernel<4, 2, true> : attn_q8_decode_kernel<4, 1, true>)
+                                                     : (wide ? attn_q8_decode_kernel<8, 2, true> : attn_q8_decode_kernel<8, 1, true>))
+                : bits == 4 ? (wide ? attn_q8_decode_kernel<4, 2> : attn_q8_decode_kernel<4, 1>)
                 : bits == 8 ? (wide ? attn_q8_decode_kernel<8, 2> : attn_q8_decode_kernel<8, 1>)
                 : a.scored  ? (wide ? attn_q8_decode_kernel<16, 2, true> : attn_q8_decode_kernel<16, 1, true>)
                             : (wide ? attn_q8_decode_kernel<16, 2> : attn_q8_decode_kernel<16, 1>);

@@ -210,7 +210,7 @@ __device__ __forceinline__ void exp_half_small(const ScoreMods &m, const uint32_
 // kEarly (bf16 rows, chunks of two row tiles): Q K^T of the next key tile is issued under the softmax of the
 // current one, see the issuer.
 // kMods (bf16 rows, no window): what a scored step does to its scores (ScoreMods).  kRanged: a range of rows per token, nothing else;
-// kCapped: a cap as well; kBiased: a bias, and a cap or none.  Capped and biased scores are brought to log2 units before the softmax.
+// kCapped: a cap as well; kBiased: a bias, a cap, both or neither (quantised storage has only this one).  Capped and biased scores are brought to log2 units before the softmax.
 // With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the line of all tiles is.
 // 256 tokens of 32 / 8 heads at prefix 31 K: plain 108 us, capped 139 (scores up to half the cap), biased XXX.
 // kRanks (bf16 rows, two streams): a cluster of that many CTAs has one row tile of one KV head, each an equal share of its key
@@ -220,6 +220,7 @@ __global__ void __launch_bounds__(kQuant ? kThreadsQ8 : kThreads, 1)
 attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v) {
     constexpr bool kScored = kMods != kPlain;
+    static_assert(kMods == kPlain || kQuant == 0 || kMods == kBiased, "quantised storage has one kernel for all scored steps");
     static_assert(!kEarly || kQuant == 0 || kPair, "the early issue needs the space of a K/V slot for its probabilities");
     constexpr int NS = kQuant ? kSlotsQ8 : kEarly ? kSlotsEarly : kSlots;        // slots behind the Q tiles: the shared ring's
     constexpr int SR = kQuant ? 2 : 3;                     // slots of each stream's own ring
@@ -342,8 +343,8 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&ctl->tmem_base);
     if constexpr (kScored) {
         if (a.mods.first || a.mods.end) {          // (uniform: the whole CTA comes here, or none of it)
-            const int tok = row0 / G + (int)threadIdx.x;            // (a row pair has 256 tokens at most)
-            if (tok <= tok_last) {
+            // (the two CTAs of a pair walk the same key tiles: those that the tokens of either see)
+            for (int tok = (kPair ? (qpair & ~1) * kCtaRows : row0) / G + (int)threadIdx.x; tok <= tok_last; tok += (int)blockDim.x) {
                 const RowRange r = seen_rows(a.mods, (int64_t)cb * nmax + tok, tok, P, L, a.self_rows);
                 if (r.begin < r.end) {
                     atomicMin(&ctl->seen[0], (int)(r.begin / kRows));
@@ -805,7 +806,8 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
             float l = 0.f;
             // (kBiased) the head's slope in log2 units per row of distance
             float slope = 0.f;
-            if (kMods == kBiased && valid) slope = a.mods.slopes[kvh * a.G + gi] * kLog2e;
+            if (kMods == kBiased && a.mods.slopes && valid) slope = a.mods.slopes[kvh * a.G + gi] * kLog2e;
+            const int64_t position = kMods == kBiased ? a.mods.position(cb, tok) : 0;
             for (int j = j0, k = 0; j < ntiles; j += jstep, ++it, ++k) {
                 ok = mbar_wait(bar(B_SFULL0 + i), it & 1, ctl, a.status);
                 ok = __all_sync(0xffffffffu, ok);
@@ -843,7 +845,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     auto put = [&](int c, float2 x) { sc[c] = __float_as_uint(x.x); sc[c + 1] = __float_as_uint(x.y); };
                     const bool cap = kMods == kCapped || a.mods.cap_out > 0.f;
                     // (kBiased) distance of the tile's first key; all of the tile's keys behind the token: the bias is a line
-                    const int64_t behind = kMods == kBiased ? a.mods.pos0 + tok - key0 : 0;
+                    const int64_t behind = kMods == kBiased ? position - key0 : 0;
                     const float at = (float)behind;
                     const bool line = kMods == kBiased && __all_sync(0xffffffffu, !valid || behind >= kRows - 1);
                     const float2 from = both(-slope * at), per = both(slope);
@@ -1593,7 +1595,8 @@ cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     static_assert(kSmemBytesQ8 <= 232448, "shared memory budget of one CTA (int8 storage)");
     static_assert(kSmemBytesPair <= 232448 && kOffCtlPair % 1024 == 0, "shared memory budget of one CTA (pairs of CTAs)");
     const bool quant = a.quant_bits != 0;
-    auto kernel = a.quant_bits == 8 ? (a.win_lo > 0 ? attn_tc_kernel<true, 8, false, false> : attn_tc_kernel<false, 8, false, false>)
+    auto kernel = a.quant_bits && a.scored ? (a.quant_bits == 8 ? attn_tc_kernel<false, 8, false, false, 0, kBiased> : attn_tc_kernel<false, 4, false, false, 0, kBiased>)
+                : a.quant_bits == 8 ? (a.win_lo > 0 ? attn_tc_kernel<true, 8, false, false> : attn_tc_kernel<false, 8, false, false>)
                 : a.quant_bits == 4 ? (a.win_lo > 0 ? attn_tc_kernel<true, 4, false, false> : attn_tc_kernel<false, 4, false, false>)
                 : a.scored && a.mods.slopes      ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kBiased> : attn_tc_kernel<false, 0, false, false, 0, kBiased>)
                 : a.scored && a.mods.cap_out > 0 ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kCapped> : attn_tc_kernel<false, 0, false, false, 0, kCapped>)
@@ -1611,7 +1614,8 @@ cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     }
     dim3 grid(attn_tc_row_pairs(a.n, a.Gp), a.ngroups, a.batch);
     if (pair_launch_ok(a)) {
-        auto paired = a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true> : attn_tc_kernel<false, 4, true, true>;
+        auto paired = a.scored ? (a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true, 0, kBiased> : attn_tc_kernel<false, 4, true, true, 0, kBiased>)
+                    : a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true> : attn_tc_kernel<false, 4, true, true>;
         cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(paired), (int)kSmemBytesPair);
         if (e != cudaSuccess) return e;
         if (pair_clusters_fit(reinterpret_cast<const void *>(paired), kSmemBytesPair))

@@ -700,7 +700,7 @@ kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void 
     ra.sms = c->sm_count;
     ra.table = c->table;
 
-    AttnArgs aa;
+    AttnArgs aa = {};
     aa.scored = scores != nullptr;
     aa.mods = score_mods(c, scores, pos0);
     aa.q_rot = ra.q_rot;
@@ -866,7 +866,7 @@ kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
     if ((sc->slopes && check_f32(sc->slopes)) || (sc->first && check_f32(reinterpret_cast<const float *>(sc->first))) ||
         (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
         return KVF_ERR_INVALID_ARG;
-    if (c->window > 0 || c->quant) return KVF_ERR_UNSUPPORTED;
+    if (c->window > 0) return KVF_ERR_UNSUPPORTED;
     return KVF_OK;
 }
 
@@ -1540,7 +1540,7 @@ __global__ void write_lengths_kernel(const LenChunk c, int64_t *prefixes, int64_
 // (ragged only): member i folds ns[i] <= n tokens (0 = it sits the step out) out of blocks of n.
 kvf_status batch_step(kvf_batch *b, const void *q, const void *k_new, const void *v_new, int32_t n,
                       int64_t pos0, const int64_t *pos0s, const int32_t *ns, void *out, float *lse,
-                      void *cuda_stream) {
+                      void *cuda_stream, const kvf_scores *scores = nullptr) {
     if (!b) return KVF_ERR_INVALID_ARG;
     kvf_cache *c0 = b->caches[0];
     const bool ragged = pos0s != nullptr;
@@ -1566,7 +1566,8 @@ kvf_status batch_step(kvf_batch *b, const void *q, const void *k_new, const void
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const kvf_config &f = c0->cfg;
     const int B = (int)b->caches.size();
-    const Plan plan = make_plan(c0, n, P, B, b->part_rows, true, ragged);
+    if (scores && (s = check_scores(c0, scores)) != KVF_OK) return s;
+    const Plan plan = make_plan(c0, n, P, B, b->part_rows, true, ragged, scores != nullptr);
     int64_t *dev_prefixes = reinterpret_cast<int64_t *>(b->workspace + b->off_lens);
     int64_t *dev_pos0s = dev_prefixes + B;
     int64_t *dev_ns = dev_pos0s + B;
@@ -1607,7 +1608,10 @@ kvf_status batch_step(kvf_batch *b, const void *q, const void *k_new, const void
     ra.sms = c0->sm_count;
     ra.table = c0->table;
 
-    AttnArgs aa;
+    AttnArgs aa = {};
+    aa.scored = scores != nullptr;
+    aa.mods = score_mods(c0, scores, pos0);
+    aa.mods.pos0s = ragged ? dev_pos0s : nullptr;
     aa.q_rot = ra.q_rot;
     aa.k_plane = ra.k_plane; aa.v_plane = ra.v_plane;
     aa.out = out; aa.lse = lse;
@@ -1688,6 +1692,25 @@ kvf_status kvf_batch_fold_step_varlen(kvf_batch *b, const void *q, const void *k
         pos0_or_null = own.data();
     }
     return batch_step(b, q, k_new, v_new, max_tokens, 0, pos0_or_null, n_tokens, out, lse, cuda_stream);
+}
+
+kvf_status kvf_batch_fold_step_scored(kvf_batch *b, const void *q, const void *k_new, const void *v_new, const int32_t *n_tokens_or_null,
+                                      int32_t max_tokens, const int64_t *pos0_or_null, const kvf_scores *scores, void *out, float *lse,
+                                      void *cuda_stream) {
+    if (!b || !scores) return KVF_ERR_INVALID_ARG;
+    // members of one length take the step of kvf_batch_fold_step, the others kvf_batch_fold_step_ragged's or _varlen's
+    bool alike = n_tokens_or_null == nullptr;
+    const int64_t len0 = b->caches[0]->len;
+    for (size_t i = 0; i < b->caches.size(); ++i)
+        alike = alike && b->caches[i]->len == len0 && (!pos0_or_null || pos0_or_null[i] == pos0_or_null[0]);
+    if (alike)
+        return batch_step(b, q, k_new, v_new, max_tokens, pos0_or_null ? pos0_or_null[0] : len0, nullptr, nullptr, out, lse, cuda_stream, scores);
+    std::vector<int64_t> own;
+    if (!pos0_or_null) {
+        for (kvf_cache *c : b->caches) own.push_back(c->len);
+        pos0_or_null = own.data();
+    }
+    return batch_step(b, q, k_new, v_new, max_tokens, 0, pos0_or_null, n_tokens_or_null, out, lse, cuda_stream, scores);
 }
 
 kvf_status kvf_batch_plan(const kvf_batch *b, int32_t n_tokens, int64_t prefix_len, int32_t plan[4]) {

@@ -139,6 +139,7 @@ struct RopeAppendArgs {
 // s - slope[head] * |position of the token - row|; token i sees rows [first[i], end[i]).
 struct ScoreMods {
     float cap_in, cap_out;           // scale / softcap and softcap * log2(e) (cap_out = 0: no cap)
+    float cap_log2;                  // 2 log2(e) / cap_out: what a score in log2 units is multiplied with on its way to e^2x
     float small_to;                  // dot products up to this go by small[]: cap_out * tanh(x) = s * (small[0] + ... + small[3] s^6)
     float small[4];                  // (s the dot product itself; see scores.cuh)
     float middle_to;                 // ... up to this by middle[]: x * (middle[0] + ... + middle[4] x^8), x = cap_in * s
@@ -146,6 +147,10 @@ struct ScoreMods {
     const float *slopes;             // device [H] or null
     const int32_t *first, *end;      // device [n] or null (row 0; every row up to the token's own)
     int64_t pos0;                    // position of token 0
+    const int64_t *pos0s;            // ragged batch: device array of the members', else null
+#ifdef __CUDACC__
+    __device__ __forceinline__ int64_t position(int member, int tok) const { return (pos0s ? pos0s[member] : pos0) + tok; }
+#endif
 };
 
 void set_score_cap(ScoreMods &m, double scale, double softcap);

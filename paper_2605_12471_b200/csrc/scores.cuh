@@ -33,6 +33,7 @@ inline void set_cap(ScoreMods &m, double scale, double softcap) {
     const double in = scale / softcap, out = softcap * 1.4426950408889634;
     m.cap_in = (float)in;
     m.cap_out = (float)out;
+    m.cap_log2 = (float)(2.0 * 1.4426950408889634 / out);
     // (powers of `in` below fp32's range, under caps of a thousand times the usual: the middle polynomial alone, which does without)
     m.small_to = in > 1e-4 ? (float)(kSmallX / in) : 0.f;
     for (int i = 0; i < 4; ++i) m.small[i] = (float)(kSmallTanh[i] * out * pow(in, 2 * i + 1));
@@ -56,6 +57,14 @@ __device__ __forceinline__ float2 cap_small_over(const ScoreMods &m, float2 s) {
 __device__ __forceinline__ float cap_any(const ScoreMods &m, float s) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * (m.cap_in * (2.f * kLog2e))));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return m.cap_out * fmaf(-2.f, r, 1.f);
+}
+
+// The same of a score already in log2 units.
+__device__ __forceinline__ float cap_log2(const ScoreMods &m, float x) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * m.cap_log2));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return m.cap_out * fmaf(-2.f, r, 1.f);
 }
