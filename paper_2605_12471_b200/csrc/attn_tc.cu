@@ -198,6 +198,18 @@ __device__ __forceinline__ void exp_half_small(const ScoreMods &m, const uint32_
     }
 }
 
+// A bias that is a line over a tile's keys: slope * key + base, eight keys at a time - what the eight differ by is kept in registers
+// (as multiply-adds with the key's number every pair of numbers has to be brought into registers first).
+struct Line {
+    float2 within[4];
+    float slope, base;
+    __device__ __forceinline__ Line(float slope_, float base_) : slope(slope_), base(base_) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) within[r] = make_float2(slope * (float)(2 * r), slope * (float)(2 * r + 1));
+    }
+    __device__ __forceinline__ float2 at(int c) const { return __fadd2_rn(within[(c >> 1) & 3], both(fmaf(slope, (float)(c & ~7), base))); }   // keys c, c + 1
+};
+
 // kWindow = false compiles the sink + window arithmetic out (launched whenever win_lo == 0).
 // kQuant (0, 8 or 4 bits): map_k / map_v describe int8 or int4 code planes; the producer brings raw code tiles into their own
 // ring and warps 12-15 (one thread per key row) expand each to the swizzled bf16 tile the MMAs read,
@@ -848,8 +860,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     const int64_t behind = kMods == kBiased ? position - key0 : 0;
                     const float at = (float)behind;
                     const bool line = kMods == kBiased && __all_sync(0xffffffffu, !valid || behind >= kRows - 1);
-                    const float2 from = both(-slope * at), per = both(slope);
-                    auto on_line = [&](int c) { return __ffma2_rn(per, make_float2((float)c, (float)(c + 1)), from); };
+                    const Line bias(slope, -slope * at);
                     bool biased = false;
                     if (cap) {
                         // what the tile's largest score in magnitude allows (rows past the chunk's end do not count)
@@ -875,7 +886,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                             } else if (kMods == kBiased && line) {
                                 biased = true;
 #pragma unroll
-                                for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), cap_small_over(a.mods, pair(c)), on_line(c)));
+                                for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), cap_small_over(a.mods, pair(c)), bias.at(c)));
                             } else {
 #pragma unroll
                                 for (int c = 0; c < 128; c += 2) put(c, __fmul2_rn(pair(c), cap_small_over(a.mods, pair(c))));
@@ -894,7 +905,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                             // (with the cap)
                         } else if (line) {
 #pragma unroll
-                            for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), by, on_line(c)));
+                            for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), by, bias.at(c)));
                         } else {
 #pragma unroll
                             for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(fmaf(__uint_as_float(sc[c]), by.x, -slope * fabsf(at - (float)c)));
