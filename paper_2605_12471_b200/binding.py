@@ -203,14 +203,14 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
-def _scores(softcap, slopes, first, end, heads: int, n: int) -> Optional[kvf_scores]:
+def _scores(softcap, slopes, first, end, heads: int, n: int, device) -> Optional[kvf_scores]:
     """kvf_scores of a step's keywords, or None where none was given (a plain step)."""
     if not softcap and slopes is None and first is None and end is None:
         return None
     if slopes is not None:
-        assert slopes.is_cuda and slopes.is_contiguous() and slopes.dtype is torch.float32 and slopes.numel() == heads
+        assert slopes.device == device and slopes.is_contiguous() and slopes.dtype is torch.float32 and slopes.numel() == heads
     for t in (first, end):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype is torch.int32 and t.numel() == n)
+        assert t is None or (t.device == device and t.is_contiguous() and t.dtype is torch.int32 and t.numel() == n)
     return kvf_scores(softcap, *(None if t is None else t.data_ptr() for t in (slopes, first, end)))
 
 
@@ -279,7 +279,7 @@ class Cache:
         n = q.shape[0]
         if out is None:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q.device)
         if scores is not None:
             rc = lib.kvf_fold_step_scored(h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), n,
                                           lib.kvf_cache_len(h) if pos0 is None else int(pos0), ctypes.byref(scores), out.data_ptr(),
@@ -304,7 +304,7 @@ class Cache:
         assert q.is_cuda and q.is_contiguous() and q.dtype == self.torch_dtype
         if out is None:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q.device)
         if scores is not None:
             rc = load().kvf_attend_scored(self._h, q.data_ptr(), n, int(len(self) if pos0 is None else pos0), ctypes.byref(scores),
                                           out.data_ptr(), lse.data_ptr() if lse is not None else None, _stream_ptr(stream))
@@ -338,14 +338,14 @@ class Cache:
         row; mass and out are [Hkv, >= len] fp32 (out may be mass; a new [Hkv, len] tensor by default)."""
         n, rows, hkv = q_rot.shape[0], len(self), self.cfg.n_kv_heads
         assert q_rot.is_cuda and q_rot.is_contiguous() and q_rot.dtype == self.torch_dtype
-        assert lse.is_cuda and lse.is_contiguous() and lse.dtype is torch.float32 and lse.numel() == n * self.cfg.n_q_heads
+        assert lse.device == q_rot.device and lse.is_contiguous() and lse.dtype is torch.float32 and lse.numel() == n * self.cfg.n_q_heads
         if out is None:
             out = torch.empty((hkv, rows), dtype=torch.float32, device=q_rot.device)
         for t in (mass, out):
-            assert t is None or (t.is_cuda and t.dtype is torch.float32 and t.dim() == 2 and t.shape[0] == hkv and t.shape[1] >= rows and t.stride(1) == 1)
+            assert t is None or (t.device == q_rot.device and t.dtype is torch.float32 and t.dim() == 2 and t.shape[0] == hkv and t.shape[1] >= rows and t.stride(1) == 1)
         if pos0 is None:
             pos0 = max(rows - n, 0) if appended else rows
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n)
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q_rot.device)
         rc = load().kvf_cache_mass(self._h, q_rot.data_ptr(), n, int(appended), int(pos0), None if scores is None else ctypes.byref(scores),
                                    lse.data_ptr(), None if mass is None else mass.data_ptr(), 0 if mass is None else mass.stride(0),
                                    decay, out.data_ptr(), out.stride(0), _stream_ptr(stream))
@@ -361,8 +361,8 @@ class Cache:
         if kept is None:
             kept = torch.empty((hkv, budget), dtype=torch.int32, device=mass.device)
         assert mass.is_cuda and mass.dtype is torch.float32 and mass.shape[0] == hkv and mass.shape[1] >= len(self) and mass.stride(1) == 1
-        assert kept.is_cuda and kept.dtype is torch.int32 and kept.is_contiguous() and kept.numel() == hkv * budget
-        assert mass_out is None or (mass_out.is_cuda and mass_out.dtype is torch.float32 and mass_out.shape[0] == hkv and
+        assert kept.device == mass.device and kept.dtype is torch.int32 and kept.is_contiguous() and kept.numel() == hkv * budget
+        assert mass_out is None or (mass_out.device == mass.device and mass_out.dtype is torch.float32 and mass_out.shape[0] == hkv and
                                     mass_out.shape[1] >= budget and mass_out.stride(1) == 1)
         rc = load().kvf_cache_evict(self._h, into._h, mass.data_ptr(), mass.stride(0), n_sink, n_recent, budget,
                                     None if mass_out is None else mass_out.data_ptr(), 0 if mass_out is None else mass_out.stride(0),
@@ -586,7 +586,7 @@ class Batch:
         length; pos0 is then None or one position per member).  With any of softcap, slopes ([H] fp32), first, end
         ([n_caches, n] int32) kvf_batch_fold_step_scored."""
         assert q.dim() == 4 and q.shape[0] == len(self.caches)
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1])
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1], q.device)
         if scores is not None:
             if pos0 is not None and not ragged:
                 pos0 = [pos0] * len(self.caches)
@@ -636,7 +636,7 @@ class Batch:
         """kvf_batch_fold_step_varlen: member i folds the first n_tokens[i] rows of its block (0 = sits out).  With any of
         softcap, slopes ([H] fp32), first, end ([n_caches, longest] int32) kvf_batch_fold_step_scored."""
         assert q.dim() == 4 and q.shape[0] == len(self.caches) == len(n_tokens)
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1])
+        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, q.shape[0] * q.shape[1], q.device)
         if scores is not None:
             return self._fold_scored(q, k_new, v_new, n_tokens, pos0, scores, out, lse, stream)
         for t in (q, k_new, v_new):

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkvfold.so")
-SOURCES = ["kvfold_api.cu", "rope_append.cu", "quant_append.cu", "attn_simt.cu", "fold_small.cu", "attn_tc.cu", "attn_tc32.cu", "attn_q8_decode.cu", "merge_parts.cu",
+SOURCES = ["kvfold_api.cu", "rope_append.cu", "quant_append.cu", "attn_simt.cu", "fold_small.cu", "attn_tc.cu", "attn_tc_scored.cu", "attn_tc32.cu", "attn_q8_decode.cu", "merge_parts.cu",
            "attn_mass.cu", "evict.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
@@ -42,7 +42,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         s = os.path.join(CSRC, src)
         o = os.path.join(OBJ, src.replace(".cu", ".o"))
         objs.append(o)
-        if force or _stale(o, [s] + headers):
+        if force or _stale(o, [s] + headers + ([os.path.join(CSRC, "attn_tc.cu")] if src == "attn_tc_scored.cu" else [])):
             jobs.append((src, [nvcc] + NVCC_FLAGS + ["-c", s, "-o", o]))
 
     def run(job):
@@ -52,7 +52,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             f.write(r.stdout + r.stderr)
         return name, r
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=4) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=os.cpu_count() or 4) as ex:
         for name, r in ex.map(run, jobs):
             if verbose or r.returncode != 0:
                 sys.stderr.write(r.stdout + r.stderr)

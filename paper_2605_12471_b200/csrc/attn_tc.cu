@@ -224,7 +224,7 @@ struct Line {
 // kMods (bf16 rows, no window): what a scored step does to its scores (ScoreMods).  kRanged: a range of rows per token, nothing else;
 // kCapped: a cap as well; kBiased: a bias, a cap, both or neither (quantised storage has only this one).  Capped and biased scores are brought to log2 units before the softmax.
 // With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the line of all tiles is.
-// 256 tokens of 32 / 8 heads at prefix 31 K: plain 108 us, capped 139 (scores up to half the cap), biased XXX.
+// 256 tokens of 32 / 8 heads at prefix 31 K: plain 108 us, capped 140 (scores up to half the cap), biased 143, both 184.
 // kRanks (bf16 rows, two streams): a cluster of that many CTAs has one row tile of one KV head, each an equal share of its key
 // tiles, and writes the output: no partial results, no merge kernel.  See the end of the kernel.
 template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0, int kMods = kPlain>
@@ -1295,6 +1295,24 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
     if (clocked) add_clock_counters(a.status, clock64() - ctl->clk0, global_ns() - ctl->ns0);
 }
 
+}  // namespace
+
+#ifdef KVF_SCORED_KERNELS
+// (attn_tc_scored.cu: a file of its own, so that these kernels are compiled beside the others)
+template <bool kEarly>
+static AttnTcKernel of_mods(const ScoreMods &m) {
+    return m.slopes ? attn_tc_kernel<false, 0, false, kEarly, 0, kBiased>
+         : m.cap_out > 0.f ? attn_tc_kernel<false, 0, false, kEarly, 0, kCapped> : attn_tc_kernel<false, 0, false, kEarly, 0, kRanged>;
+}
+AttnTcKernel scored_attn_tc_kernel(const AttnArgs &a, bool pair) {
+    if (a.quant_bits == 8) return pair ? attn_tc_kernel<false, 8, true, true, 0, kBiased> : attn_tc_kernel<false, 8, false, false, 0, kBiased>;
+    if (a.quant_bits == 4) return pair ? attn_tc_kernel<false, 4, true, true, 0, kBiased> : attn_tc_kernel<false, 4, false, false, 0, kBiased>;
+    return a.streams == 1 ? of_mods<true>(a.mods) : of_mods<false>(a.mods);
+}
+void set_score_cap(ScoreMods &m, double scale, double softcap) { set_cap(m, scale, softcap); }
+#else
+namespace {
+
 // One merged row: lane = float4 column, `den` and `M` as below.
 __device__ __forceinline__ void write_merged(const AttnArgs &a, int cb, int kvh, int tok, int gi, int lane, float4 acc, float den, float M) {
     const int64_t row = ((int64_t)cb * a.n + tok) * a.H + kvh * a.G + gi;
@@ -1598,20 +1616,15 @@ int attn_tc_row_ranks(int units, int sms, int64_t key_tiles) {
     return units <= sms && key_tiles <= 46 * (int64_t)units / sms - 10 ? 1 : 0;
 }
 
-void set_score_cap(ScoreMods &m, double scale, double softcap) { set_cap(m, scale, softcap); }
-
 cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s) {
     static_assert(sizeof(Ctl) <= 512, "control block");
     static_assert(kSmemBytes <= 232448, "shared memory budget of one CTA");
     static_assert(kSmemBytesQ8 <= 232448, "shared memory budget of one CTA (int8 storage)");
     static_assert(kSmemBytesPair <= 232448 && kOffCtlPair % 1024 == 0, "shared memory budget of one CTA (pairs of CTAs)");
     const bool quant = a.quant_bits != 0;
-    auto kernel = a.quant_bits && a.scored ? (a.quant_bits == 8 ? attn_tc_kernel<false, 8, false, false, 0, kBiased> : attn_tc_kernel<false, 4, false, false, 0, kBiased>)
+    auto kernel = a.scored          ? scored_attn_tc_kernel(a, false)
                 : a.quant_bits == 8 ? (a.win_lo > 0 ? attn_tc_kernel<true, 8, false, false> : attn_tc_kernel<false, 8, false, false>)
                 : a.quant_bits == 4 ? (a.win_lo > 0 ? attn_tc_kernel<true, 4, false, false> : attn_tc_kernel<false, 4, false, false>)
-                : a.scored && a.mods.slopes      ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kBiased> : attn_tc_kernel<false, 0, false, false, 0, kBiased>)
-                : a.scored && a.mods.cap_out > 0 ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kCapped> : attn_tc_kernel<false, 0, false, false, 0, kCapped>)
-                : a.scored                       ? (a.streams == 1 ? attn_tc_kernel<false, 0, false, true, 0, kRanged> : attn_tc_kernel<false, 0, false, false, 0, kRanged>)
                                     : a.streams == 1      ? (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, true> : attn_tc_kernel<false, 0, false, true>)
                                     : (a.win_lo > 0 ? attn_tc_kernel<true, 0, false, false> : attn_tc_kernel<false, 0, false, false>);
     const uint32_t smem = quant ? kSmemBytesQ8 : kSmemBytes;
@@ -1625,8 +1638,7 @@ cudaError_t launch_attn_tc(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     }
     dim3 grid(attn_tc_row_pairs(a.n, a.Gp), a.ngroups, a.batch);
     if (pair_launch_ok(a)) {
-        auto paired = a.scored ? (a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true, 0, kBiased> : attn_tc_kernel<false, 4, true, true, 0, kBiased>)
-                    : a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true> : attn_tc_kernel<false, 4, true, true>;
+        auto paired = a.scored ? scored_attn_tc_kernel(a, true) : a.quant_bits == 8 ? attn_tc_kernel<false, 8, true, true> : attn_tc_kernel<false, 4, true, true>;
         cudaError_t e = raise_smem_limit_once(reinterpret_cast<const void *>(paired), (int)kSmemBytesPair);
         if (e != cudaSuccess) return e;
         if (pair_clusters_fit(reinterpret_cast<const void *>(paired), kSmemBytesPair))
@@ -1664,5 +1676,7 @@ cudaError_t launch_combine_groups(const AttnArgs &a, int sms, cudaStream_t s) {
     if (few) return launch_pdl(combine_groups_kernel<true>, grid, dim3(256), 0, s, a);
     return launch_pdl(combine_groups_kernel<false>, grid, dim3(256), 0, s, a);
 }
+
+#endif
 
 }  // namespace kvf

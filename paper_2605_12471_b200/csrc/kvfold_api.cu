@@ -861,7 +861,16 @@ size_t page_bytes_of(const kvf_config *cfg) {
 
 kvf_status check_f32(const float *p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3u) ? KVF_ERR_INVALID_ARG : KVF_OK; }
 
+// Whether the device that is current is the one the cache lives on.
+kvf_status on_device(const kvf_cache *c) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+    return dev == c->device ? KVF_OK : KVF_ERR_INVALID_ARG;
+}
+
 kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
+    if (const kvf_status s = on_device(c)) return s;
     if (!sc || !(sc->softcap >= 0.0) || std::isinf(sc->softcap)) return KVF_ERR_INVALID_ARG;
     if ((sc->slopes && check_f32(sc->slopes)) || (sc->first && check_f32(reinterpret_cast<const float *>(sc->first))) ||
         (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
@@ -1070,6 +1079,7 @@ kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int
     if (!c) return KVF_ERR_INVALID_ARG;
     if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0) return KVF_ERR_INVALID_ARG;
     if (check_ptr(q) || check_ptr(q_rot)) return KVF_ERR_INVALID_ARG;
+    if (const kvf_status s = on_device(c)) return s;
     const kvf_config &f = c->cfg;
     if (overlap(q, q_rot, (size_t)n_tokens * f.n_q_heads * f.head_dim * elem_bytes(f.dtype)) && q != q_rot) return KVF_ERR_INVALID_ARG;
     RopeAppendArgs ra = {};
@@ -1095,6 +1105,7 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     if (appended && n_tokens > c->len) return KVF_ERR_INVALID_ARG;
     if (!std::isfinite(decay)) return KVF_ERR_INVALID_ARG;
     if (c->quant || c->window > 0) return KVF_ERR_UNSUPPORTED;
+    if (const kvf_status s = on_device(c)) return s;
     if (scores) {
         const kvf_status s = check_scores(c, scores);
         if (s != KVF_OK) return s;
@@ -1160,6 +1171,10 @@ kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *ma
     if (check_f32(mass) || (mass_out && check_f32(mass_out)) || check_f32(reinterpret_cast<const float *>(kept))) return KVF_ERR_INVALID_ARG;
     if (mass_stride < from->len || (mass_out && out_stride < budget)) return KVF_ERR_INVALID_ARG;
     if (mass_out && overlap(mass, strided_bytes(from, mass_stride), mass_out, strided_bytes(from, out_stride))) return KVF_ERR_INVALID_ARG;
+    const size_t kept_bytes = (size_t)x.n_kv_heads * (size_t)budget * 4;
+    if (overlap(mass, strided_bytes(from, mass_stride), kept, kept_bytes) || (mass_out && overlap(mass_out, strided_bytes(from, out_stride), kept, kept_bytes)))
+        return KVF_ERR_INVALID_ARG;
+    if (const kvf_status s = on_device(from)) return s;
     // two paged caches of one pool keep different pages of it (the caller's tables say so); nothing else may be shared
     if (!(from->page_table && to->page_table && from->storage == to->storage && from->page_table != to->page_table) &&
         overlap(from->storage, held_bytes(from), to->storage, held_bytes(to)))

@@ -139,7 +139,7 @@ struct RopeAppendArgs {
 // s - slope[head] * |position of the token - row|; token i sees rows [first[i], end[i]).
 struct ScoreMods {
     float cap_in, cap_out;           // scale / softcap and softcap * log2(e) (cap_out = 0: no cap)
-    float cap_log2;                  // 2 log2(e) / cap_out: what a score in log2 units is multiplied with on its way to e^2x
+    float cap_log2;                  // 1 / cap_out: a score in log2 units over the cap
     float small_to;                  // dot products up to this go by small[]: cap_out * tanh(x) = s * (small[0] + ... + small[3] s^6)
     float small[4];                  // (s the dot product itself; see scores.cuh)
     float middle_to;                 // ... up to this by middle[]: x * (middle[0] + ... + middle[4] x^8), x = cap_in * s
@@ -281,6 +281,8 @@ struct TcMaps {
     CUtensorMap q, k, v;
     CUtensorMap k_half, v_half;      // quantised storage: boxes of half a key tile's rows, for the pairs of CTAs
 };
+using AttnTcKernel = void (*)(AttnArgs, CUtensorMap, CUtensorMap, CUtensorMap);
+AttnTcKernel scored_attn_tc_kernel(const AttnArgs &a, bool pair);      // of a scored step (attn_tc_scored.cu); pair: on pairs of CTAs
 bool attn_tc_supported(int dtype, int d, int G);
 int attn_tc_padded_group(int G);       // G rounded up to a power of two: rows a token takes in the tcgen05 kernels' row layout
 int attn_tc_row_pairs(int n, int G);   // 256-row pairs per KV head (G: the padded group, as below)

@@ -320,3 +320,78 @@ def test_captured_mass_and_eviction_replay_on_new_weights():
         assert torch.equal(out, src.mass(q, lse, mass=mass))
         assert torch.equal(kept.cpu(), scored.kept_rows(out, 900, 4, 64, 500))
         same_rows(src, dst, kept)
+
+
+def test_a_denominator_that_is_nan_reaches_the_rows_its_token_sees_and_no_others():
+    for heads, dtype in (((32, 8, 128), "bf16"), ((8, 2, 64), "f32")):
+        for n in (1, 200):
+            cache, gen = make(heads, dtype, 600, n, prefix=600, seed=1)
+            q = chunk(cache, gen, n)[0]
+            lse = torch.randn((n, heads[0]), generator=gen, device="cuda") + 7
+            lse[0, 0] = math.nan
+            first = torch.zeros(n, dtype=torch.int32, device="cuda")
+            first[0] = 150
+            mass = cache.mass(q, lse, first=first)
+            seen = torch.arange(600, device="cuda")
+            assert torch.equal(torch.isnan(mass[0]), (seen >= 150) & (seen <= 600 - n))
+            assert not bool(torch.isnan(mass[1:]).any())
+
+
+def test_mass_of_a_whole_large_chunk_in_many_splits():
+    """Few keys and many queries: the query tiles are split over CTAs, whose sums are added in order."""
+    cache, gen = make((16, 2, 128), "bf16", 3000, 2900, prefix=2900, seed=2)
+    q = chunk(cache, gen, 2900)[0]
+    keys = cache.k_plane()[:, :2900]
+    seen = scored.ranges(2900, 2900, 0, True)
+    lse = torch.cat([lse_of(q[a:a + 500].double(), keys, (seen[0][a:a + 500], seen[1][a:a + 500]), 1 / math.sqrt(128), a) for a in range(0, 2900, 500)])
+    got = cache.mass(q, lse)
+    want, off = 0, 0
+    for a in range(0, 2900, 500):
+        w, o = scored.mass(q[a:a + 500], keys, lse[a:a + 500], (seen[0][a:a + 500], seen[1][a:a + 500]), 1 / math.sqrt(128), a)
+        want, off = want + w, off + o
+    assert bool(((got.double() - want).abs() <= off + 2900 * 8 * 2.0 ** -24 * want).all())
+    assert torch.equal(got, cache.mass(q, lse))
+
+
+def test_refusals():
+    src, gen = make((8, 2, 128), "bf16", 700, 64, prefix=500)
+    dst, _ = make((8, 2, 128), "bf16", 300, 1)
+    q = chunk(src, gen, 20)[0]
+    lse = torch.zeros((20, 8), device="cuda")
+    mass = torch.zeros((2, 700), device="cuda")
+
+    def refused(code, f):
+        with pytest.raises(binding.KvfError) as e:
+            f()
+        assert e.value.code == code and len(src) == 500 and len(dst) == 0
+
+    invalid, cap, unsupported = binding.KVF_ERR_INVALID_ARG, binding.KVF_ERR_CAPACITY, binding.KVF_ERR_UNSUPPORTED
+    refused(invalid, lambda: src.evict(src, mass, 100))
+    refused(invalid, lambda: src.evict(dst, mass, 501))                        # more than there are
+    refused(cap, lambda: src.evict(dst, mass, 301))                            # more than there is room for
+    refused(invalid, lambda: src.evict(dst, mass, 100, n_sink=60, n_recent=41))
+    refused(invalid, lambda: src.evict(dst, mass, 100, n_sink=-1))
+    refused(invalid, lambda: src.evict(dst, mass, 100, mass_out=mass))         # over what is read
+    refused(invalid, lambda: src.evict(dst, mass, 100, kept=mass.view(torch.int32).view(-1)[:200].view(2, 100)))
+    for other in (make((8, 2, 64), "bf16", 300, 1)[0], make((8, 2, 128), "f32", 300, 1)[0], make((8, 4, 128), "bf16", 300, 1)[0],
+                  binding.Cache(binding.make_config(8, 2, 128, "bf16", 300, 1, flags=binding.KVF_CACHE_INT8))):
+        refused(invalid, lambda: src.evict(other, mass, 100))
+    refused(invalid, lambda: src.mass(q, lse, mass=mass[:, 1:], out=mass))     # shifted in place
+    for decay in (math.nan, math.inf):
+        refused(invalid, lambda: src.mass(q, lse, mass=mass, decay=decay))
+    refused(invalid, lambda: src.mass(chunk(src, gen, 65)[0], torch.zeros((65, 8), device="cuda")))       # chunks of 64
+    refused(invalid, lambda: src.mass(q, lse, softcap=-2.0))
+    refused(invalid, lambda: src.rotate(q, pos0=-1))
+    src.set_window(4, 100)
+    refused(unsupported, lambda: src.mass(q, lse))
+    src.set_window(0, 0)
+    coded = binding.Cache(binding.make_config(8, 2, 128, "bf16", 300, 64, flags=binding.KVF_CACHE_INT8))
+    coded.set_len(100)
+    refused(unsupported, lambda: coded.mass(q, lse))
+    with pytest.raises(AssertionError):
+        src.mass(q, lse, mass=mass[:, :499])
+    with pytest.raises(AssertionError):
+        src.evict(dst, mass.double(), 100)
+    short, _ = make((8, 2, 128), "bf16", 700, 64, prefix=10)
+    with pytest.raises(binding.KvfError):
+        short.mass(q, lse)                                                     # 20 tokens appended to 10 rows

@@ -190,3 +190,96 @@ def test_repeated_steps_give_the_same_bits():
         q, k, v = chunk(cache, gen, n)
         got.append(cache.fold_step(q, k, v, softcap=15.0, slopes=slopes_of(32)))
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("softcap", [1e-3, 0.5, 300.0, 1e5, 1e9])
+@pytest.mark.parametrize("n", [1, 5, 40, 200])
+def test_caps_of_every_size(softcap, n):
+    prefix = 300
+    cache, gen = make((32, 8, 128), "bf16", 600, n, prefix=prefix, seed=21)
+    q, k, v = chunk(cache, gen, n, scale=2.0)
+    lse = torch.empty((n, 32), device="cuda")
+    out = cache.fold_step(q, k, v, lse=lse, softcap=softcap)
+    # (a cap far above the scores leaves them as they are but for the polynomial's 2^-20 of the score itself)
+    want, want_lse, bound, lse_bound = scored.attend(
+        scored.turned(q, prefix, BASE), cache.k_plane()[:, :prefix + n], cache.v_plane()[:, :prefix + n], scored.ranges(n, prefix + n, prefix, True),
+        1 / math.sqrt(128), prefix, softcap)
+    plain = scored.attend(scored.turned(q, prefix, BASE), cache.k_plane()[:, :prefix + n], cache.v_plane()[:, :prefix + n],
+                          scored.ranges(n, prefix + n, prefix, True), 1 / math.sqrt(128), prefix)
+    if softcap >= 1e5:
+        bound = plain[2] + 2.0 ** -18 * 20 * plain[0].abs() + 2.0 ** -14       # (scores reach 20 here: 2^-20 * 20 * log2(e) each)
+    assert bool(((out.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("n", [1, 3, 40, 300])
+@pytest.mark.parametrize("pos0", [0, 250, 10000])
+def test_biases_of_tokens_before_among_and_behind_the_rows(n, pos0):
+    prefix = 500
+    for kw in (dict(slopes=slopes_of(32)), dict(slopes=-slopes_of(32) / 16, softcap=8.0), dict(slopes=slopes_of(32) * 40)):
+        cache, gen = make((32, 8, 128), "bf16", 900, n, prefix=prefix, seed=12)
+        q, k, v = chunk(cache, gen, n)
+        lse = torch.empty((n, 32), device="cuda")
+        out = cache.fold_step(q, k, v, pos0=pos0, lse=lse, **kw)
+        check(cache, q, k, v, n, True, lse, out, pos0, **kw)
+
+
+@pytest.mark.parametrize("heads", [(64, 1, 128), (12, 2, 128), (5, 5, 128), (6, 1, 64)])
+def test_groups_of_every_size(heads):
+    for n in (1, 2, 37, 130):
+        cache, gen = make(heads, "bf16", 700, n, prefix=400, seed=n)
+        q, k, v = chunk(cache, gen, n)
+        kw = mods_of("all", heads[0], n, 400, gen)
+        lse = torch.empty((n, heads[0]), device="cuda")
+        out = cache.fold_step(q, k, v, lse=lse, **kw)
+        check(cache, q, k, v, n, True, lse, out, 400, **kw)
+
+
+def test_scored_steps_with_the_merge_behind_them():
+    n, prefix = 64, 2000
+    cache, gen = make((32, 8, 128), "bf16", 3000, n, flags=binding.KVF_COMBINE_BEHIND, prefix=prefix, seed=5)
+    steps = []
+    for t in range(5):
+        q, k, v = chunk(cache, gen, n)
+        lse = torch.empty((n, 32), device="cuda")
+        out = cache.fold_step(q, k, v, lse=lse, softcap=9.0, slopes=slopes_of(32))
+        if t == 2:                              # the weights are added up beside an open merge: it reads partial results of its own
+            cache.mass(cache.rotate(q), torch.zeros((n, 32), device="cuda") + 9, softcap=9.0)
+        steps.append((q, out, lse, len(cache)))
+    cache.flush()
+    for q, out, lse, rows in steps:
+        cache.set_len(rows)
+        check(cache, q, None, None, n, True, lse, out, rows - n, softcap=9.0, slopes=slopes_of(32))
+
+
+def test_refusals():
+    cache, gen = make((32, 8, 128), "bf16", 600, 64, prefix=300)
+    q, k, v = chunk(cache, gen, 40)
+
+    def refused(code, f):
+        rows, count = len(cache), cache.launch_count()
+        with pytest.raises(binding.KvfError) as e:
+            f()
+        assert e.value.code == code and len(cache) == rows and cache.launch_count() == count
+
+    invalid = binding.KVF_ERR_INVALID_ARG
+    for cap in (-1.0, math.nan, math.inf):
+        refused(invalid, lambda: cache.fold_step(q, k, v, softcap=cap))
+        refused(invalid, lambda: cache.attend(q, softcap=cap))
+    refused(invalid, lambda: cache.fold_step(q, k, v, softcap=1.0, pos0=-1))
+    refused(invalid, lambda: cache.attend(torch.cat([q, q]), softcap=1.0))                       # 80 tokens, chunks of 64
+    cache.set_len(580)
+    refused(binding.KVF_ERR_CAPACITY, lambda: cache.fold_step(q, k, v, softcap=1.0))
+    cache.set_len(0)
+    refused(invalid, lambda: cache.attend(q, softcap=1.0))
+    cache.set_len(300)
+    cache.set_window(4, 100)
+    refused(binding.KVF_ERR_UNSUPPORTED, lambda: cache.fold_step(q, k, v, softcap=1.0))
+    refused(binding.KVF_ERR_UNSUPPORTED, lambda: cache.attend(q, softcap=1.0))
+    cache.set_window(0, 0)
+    with pytest.raises(AssertionError):
+        cache.fold_step(q, k, v, first=torch.zeros(39, dtype=torch.int32, device="cuda"))
+    with pytest.raises(AssertionError):
+        cache.fold_step(q, k, v, slopes=torch.zeros(32, device="cuda", dtype=torch.bfloat16))
+    with pytest.raises(AssertionError):
+        cache.fold_step(q, k, v, slopes=torch.zeros(32))
+    assert cache.status() == binding.KVF_OK
