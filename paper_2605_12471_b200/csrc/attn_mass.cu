@@ -411,7 +411,7 @@ mass_tc_kernel(const MassArgs a, const MassWork w, const int ncols, const __grid
                                 for (int t = 0; t < NK; ++t)
 #pragma unroll
                                     for (int c = 0; c < C; c += 2) {
-                                        const float2 y = middle ? cap_middle(a.mods, dot(t, c)) : make_float2(cap_any(a.mods, dot(t, c).x), cap_any(a.mods, dot(t, c).y));
+                                        const float2 y = middle ? cap_middle(a.mods, dot(t, c)) : make_float2(cap_far(a.mods, dot(t, c).x * a.mods.cap_in), cap_far(a.mods, dot(t, c).y * a.mods.cap_in));
                                         v[t][c] = __float_as_uint(y.x);
                                         v[t][c + 1] = __float_as_uint(y.y);
                                     }

@@ -896,7 +896,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                             for (int c = 0; c < 128; c += 2) put(c, cap_middle(a.mods, pair(c)));
                         } else {
 #pragma unroll
-                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(cap_any(a.mods, __uint_as_float(sc[c])));
+                            for (int c = 0; c < 128; ++c) sc[c] = __float_as_uint(cap_far(a.mods, __uint_as_float(sc[c]) * a.mods.cap_in));
                         }
                     }
                     if constexpr (kMods == kBiased) {

@@ -54,15 +54,19 @@ __device__ __forceinline__ float2 cap_small_over(const ScoreMods &m, float2 s) {
     const float2 u = __fmul2_rn(s, s);
     return __ffma2_rn(u, __ffma2_rn(u, __ffma2_rn(u, both(m.small[3]), both(m.small[2])), both(m.small[1])), both(m.small[0]));
 }
-// One score, wherever it lies (x = score / softcap).  Small ones by the polynomial here too: next to them the error of the other way,
-// 2^-23 of the cap, would grow with the cap.
-__device__ __forceinline__ float cap_of(const ScoreMods &m, float x) {
-    const float u = x * x;
-    const float y = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, m.middle[4], m.middle[3]), m.middle[2]), m.middle[1]), m.middle[0]);
+// x = score / softcap, of a tile where some lie beyond the polynomials
+__device__ __forceinline__ float cap_far(const ScoreMods &m, float x) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * (2.f * kLog2e)));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    return fabsf(x) <= kMiddleX ? y : m.cap_out * fmaf(-2.f, r, 1.f);
+    return m.cap_out * fmaf(-2.f, r, 1.f);
+}
+// One score, wherever it lies.  Small ones by the polynomial here too: next to them the error of the other way, 2^-22 of the cap, would
+// grow with the cap.
+__device__ __forceinline__ float cap_of(const ScoreMods &m, float x) {
+    const float u = x * x;
+    const float y = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, m.middle[4], m.middle[3]), m.middle[2]), m.middle[1]), m.middle[0]);
+    return fabsf(x) <= kMiddleX ? y : cap_far(m, x);
 }
 __device__ __forceinline__ float cap_any(const ScoreMods &m, float s) { return cap_of(m, s * m.cap_in); }        // of a dot product
 __device__ __forceinline__ float cap_log2(const ScoreMods &m, float y) { return cap_of(m, y * m.cap_log2); }      // of a score in log2 units
