@@ -259,7 +259,7 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  * first and end out of range mean the nearest row there is.  A token whose range is empty gets zeros and a
  * log-sum-exp of -inf.  (The paper's models have plain scores; a chunk of the fold under a cap, a bias or such a mask is
  * the same step, Section 2.)
- *   softcap  >= 0 and finite, 0 = none       slopes   device, [n_q_heads] fp32, or NULL
+ *   softcap  0 = none, else 1e-30 to 1e30, the softmax scale over it 1e-32 to 1e32       slopes   device, [n_q_heads] fp32, or NULL
  *   first    device, [n_tokens] int32, or NULL       end      device, [n_tokens] int32, or NULL
  * The device arrays are read in stream order and may be changed behind the call.  Everything else - rows appended whatever the ranges
  * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend, on every storage.  Not under a sink +

@@ -871,7 +871,11 @@ kvf_status on_device(const kvf_cache *c) {
 
 kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
     if (const kvf_status s = on_device(c)) return s;
-    if (!sc || !(sc->softcap >= 0.0) || std::isinf(sc->softcap)) return KVF_ERR_INVALID_ARG;
+    if (!sc || !(sc->softcap >= 0.0)) return KVF_ERR_INVALID_ARG;
+    if (sc->softcap > 0.0) {                 // the cap, and scores as parts of it, are fp32
+        const double part = c->scale_log2 * 0.6931471805599453 / sc->softcap;
+        if (sc->softcap < 1e-30 || sc->softcap > 1e30 || part < 1e-32 || part > 1e32) return KVF_ERR_INVALID_ARG;
+    }
     if ((sc->slopes && check_f32(sc->slopes)) || (sc->first && check_f32(reinterpret_cast<const float *>(sc->first))) ||
         (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
         return KVF_ERR_INVALID_ARG;

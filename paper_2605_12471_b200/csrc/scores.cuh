@@ -34,9 +34,11 @@ inline void set_cap(ScoreMods &m, double scale, double softcap) {
     m.cap_in = (float)in;
     m.cap_out = (float)out;
     m.cap_log2 = (float)(1.0 / out);
-    // (powers of `in` below fp32's range, under caps of a thousand times the usual: the middle polynomial alone, which does without)
-    m.small_to = in > 1e-4 ? (float)(kSmallX / in) : 0.f;
-    for (int i = 0; i < 4; ++i) m.small[i] = (float)(kSmallTanh[i] * out * pow(in, 2 * i + 1));
+    // (powers of `in` outside fp32's range, under caps of a thousand times the usual and far below it: the middle polynomial alone, which
+    // does without; tiles of zeros still come by, and zero times these has to be zero)
+    const bool powers = in > 1e-4 && in < 1e4;
+    m.small_to = powers ? (float)(kSmallX / in) : 0.f;
+    for (int i = 0; i < 4; ++i) m.small[i] = powers ? (float)(kSmallTanh[i] * out * pow(in, 2 * i + 1)) : 0.f;
     m.middle_to = (float)(kMiddleX / in);
     for (int i = 0; i < 5; ++i) m.middle[i] = (float)(kMiddleTanh[i] * out);
 }

@@ -211,6 +211,33 @@ def test_caps_of_every_size(softcap, n):
     assert bool(((out.double() - want).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("softcap", [1e-25, 1e-12, 1e-8, 1e20])
+@pytest.mark.parametrize("n", [1, 40, 200])
+@pytest.mark.parametrize("size", [0.0, 1.0])
+def test_caps_whose_powers_leave_the_range_of_fp32(softcap, n, size):
+    prefix = 700
+    cache, gen = make((32, 8, 128), "bf16", 1000, n, prefix=prefix, seed=14)
+    q, k, v = chunk(cache, gen, n)
+    q = q * size                                   # (no query at all: every score is zero)
+    lse = torch.empty((n, 32), device="cuda")
+    out = cache.fold_step(q, k, v, lse=lse, softcap=softcap)
+    # a cap far above the scores leaves them, one far below makes all rows alike
+    check(cache, q, k, v, n, True, lse, out, prefix, softcap=0.0 if softcap > 1.0 else softcap)
+    mass = cache.mass(cache.rotate(q), lse, softcap=softcap)
+    assert float((mass.double().sum(1) - 4 * n).abs().max()) <= 1e-4 * 4 * n
+
+
+def test_caps_beyond_the_range_of_fp32_are_refused():
+    cache, gen = make((32, 8, 128), "bf16", 600, 64, prefix=300)
+    q, k, v = chunk(cache, gen, 4)
+    lse = torch.zeros((4, 32), device="cuda")
+    for softcap in (1e-300, 1e-40, 1e31, 1e300):
+        for f in (lambda: cache.fold_step(q, k, v, softcap=softcap), lambda: cache.attend(q, softcap=softcap), lambda: cache.mass(q, lse, softcap=softcap)):
+            with pytest.raises(binding.KvfError) as e:
+                f()
+            assert e.value.code == binding.KVF_ERR_INVALID_ARG and len(cache) == 300
+
+
 @pytest.mark.parametrize("n", [1, 3, 40, 300])
 @pytest.mark.parametrize("pos0", [0, 250, 10000])
 def test_biases_of_tokens_before_among_and_behind_the_rows(n, pos0):
