@@ -297,7 +297,8 @@ kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int
  *   mass_out   device, [n_kv_heads][out_stride] fp32: rows [0, kvf_cache_len) of each head are written, the others left alone.
  *              May be mass_in (with the same stride), must not overlap it otherwise.  Strides >= kvf_cache_len
  * Sums are fp32 and their order depends on shapes alone.  Not on quantised storage and not under a sink + window mask
- * (KVF_ERR_UNSUPPORTED).  Asynchronous on cuda_stream; uses the cache's workspace as a step does.
+ * (KVF_ERR_UNSUPPORTED).  Asynchronous on cuda_stream; uses the cache's workspace as a step does.  Under KVF_COMBINE_BEHIND it waits for
+ * an open merge (which writes lse) as kvf_cache_flush does, and like it refuses one of another capture (KVF_ERR_INVALID_ARG).
  */
 kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int32_t appended, int64_t pos0, const kvf_scores *scores,
                           const float *lse, const float *mass_in, int64_t in_stride, float decay, float *mass_out, int64_t out_stride,

@@ -1121,6 +1121,14 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     if (mass_in && !(mass_in == mass_out && in_stride == out_stride) &&
         overlap(mass_in, strided_bytes(c, in_stride), mass_out, strided_bytes(c, out_stride)))
         return KVF_ERR_INVALID_ARG;
+    // the denominators may be those of a step whose merge is still under way
+    if (c->comb_pending) {
+        unsigned long long capture = 0;
+        kvf_status s = capture_of(static_cast<cudaStream_t>(cuda_stream), &capture);
+        if (s == KVF_OK && capture != c->comb_capture) s = KVF_ERR_INVALID_ARG;
+        if (s == KVF_OK) s = join_combine(c, static_cast<cudaStream_t>(cuda_stream));
+        if (s != KVF_OK) return s;
+    }
     MassArgs a = {};
     a.q_rot = q_rot;
     a.k_plane = c->storage;
@@ -1140,8 +1148,7 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     a.scored = scores != nullptr;
     a.mods = score_mods(c, scores, pos0);
     a.sms = c->sm_count;
-    // (the set of partial results that the next step writes: an open merge may still be reading the other)
-    a.parts = reinterpret_cast<float *>(c->workspace + (c->comb_stream && c->part_set == 1 ? c->lay.part_o2 : c->lay.part_o));
+    a.parts = reinterpret_cast<float *>(c->workspace + c->lay.part_o);          // (no merge is reading it: see above)
     a.parts_cap = c->part_rows_cap * f.head_dim;
     const PdlScope pdl(dependent_launches());
     cudaError_t e;

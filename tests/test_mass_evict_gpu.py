@@ -353,6 +353,37 @@ def test_mass_of_a_whole_large_chunk_in_many_splits():
     assert torch.equal(got, cache.mass(q, lse))
 
 
+def test_weights_behind_a_step_whose_merge_is_open():
+    n, prefix = 256, 20000
+    got, held = [], []
+    for flags in (0, binding.KVF_COMBINE_BEHIND):
+        cache, gen = make((32, 8, 128), "bf16", 24000, n, flags=flags, prefix=prefix, seed=6)
+        for _ in range(8):
+            q, k, v = chunk(cache, gen, n)
+            lse = torch.full((n, 32), math.nan, device="cuda")       # (what is read before the merge has written it stays NaN)
+            q_rot = cache.rotate(q, pos0=len(cache))
+            held.append((cache.fold_step(q, k, v, lse=lse), lse))    # (results belong to the library while their merge is open)
+            got.append(cache.mass(q_rot, lse))
+        cache.flush()
+        torch.cuda.synchronize()
+    for a, b in zip(got[:8], got[8:]):
+        assert torch.equal(a, b)
+    # a merge left open outside a capture is not joined inside it
+    q, k, v = chunk(cache, gen, n)
+    q_rot, out = cache.rotate(q, pos0=len(cache)), torch.empty((8, 24000), device="cuda")
+    held.append(cache.fold_step(q, k, v, lse=lse))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    count = cache.launch_count()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(binding.KvfError) as e:
+            cache.mass(q_rot, lse, out=out)
+    assert e.value.code == binding.KVF_ERR_INVALID_ARG and cache.launch_count() == count
+    cache.flush()
+    torch.cuda.synchronize()
+
+
 def test_refusals():
     src, gen = make((8, 2, 128), "bf16", 700, 64, prefix=500)
     dst, _ = make((8, 2, 128), "bf16", 300, 1)
