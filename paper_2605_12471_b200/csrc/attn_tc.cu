@@ -852,6 +852,7 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 tmem_wait_ld();
                 bool in_place = true;          // (kCapped) the scores in sc are what the softmax takes; else small[] is yet to come
                 float m_small = 0.f;
+                const int from = kScored ? (int)max((int64_t)0, min((int64_t)kRows, begin_s - key0)) : 0;      // columns below it are hidden
                 if constexpr (kMods >= kCapped) {
                     auto pair = [&](int c) { return make_float2(__uint_as_float(sc[c]), __uint_as_float(sc[c + 1])); };
                     auto put = [&](int c, float2 x) { sc[c] = __float_as_uint(x.x); sc[c + 1] = __float_as_uint(x.y); };
@@ -864,21 +865,32 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                     bool biased = false;
                     if (cap) {
                         // what the tile's largest score in magnitude allows (rows past the chunk's end do not count)
-                        float hi[4], lo[4];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            hi[q] = fmaxf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
-                            lo[q] = fminf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
-                        }
-#pragma unroll
-                        for (int c = 8; c < 128; c += 8)
+                        float top;
+                        auto largest = [&]() {
+                            float hi[4], lo[4];
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                hi[q] = max3(hi[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
-                                lo[q] = min3(lo[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
+                                hi[q] = fmaxf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
+                                lo[q] = fminf(__uint_as_float(sc[2 * q]), __uint_as_float(sc[2 * q + 1]));
                             }
-                        const float top = fmaxf(max3(hi[0], hi[1], hi[2]), hi[3]), low = fminf(min3(lo[0], lo[1], lo[2]), lo[3]);
-                        const float far = valid ? fmaxf(top, -low) : 0.f;
+#pragma unroll
+                            for (int c = 8; c < 128; c += 8)
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    hi[q] = max3(hi[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
+                                    lo[q] = min3(lo[q], __uint_as_float(sc[c + 2 * q]), __uint_as_float(sc[c + 2 * q + 1]));
+                                }
+                            top = fmaxf(max3(hi[0], hi[1], hi[2]), hi[3]);
+                            return valid ? fmaxf(top, -fminf(min3(lo[0], lo[1], lo[2]), lo[3])) : 0.f;
+                        };
+                        float far = largest();
+                        if (masked && __any_sync(0xffffffffu, far > a.mods.small_to)) {
+                            // Hidden columns have no say in which formula the visible ones take: a hidden row may hold anything, what an
+                            // earlier use of the cache left behind its end among it.  (Where all are small, so are the visible ones.)
+#pragma unroll
+                            for (int c = 0; c < 128; ++c) sc[c] = c >= from && c < nvis ? sc[c] : 0u;
+                            far = largest();
+                        }
                         if (!__any_sync(0xffffffffu, far > a.mods.small_to)) {
                             if (kMods == kCapped && !masked) {
                                 in_place = false;
@@ -914,7 +926,6 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap map_q, cons
                 }
                 if constexpr (kScored) {
                     // a row sees [begin_s, limit_s): what lies before it and behind it, if a row of the warp has any
-                    const int from = (int)max((int64_t)0, min((int64_t)kRows, begin_s - key0));
                     if (masked && __any_sync(0xffffffffu, nvis < kRows))
 #pragma unroll
                         for (int c = 0; c < 128; ++c) sc[c] = c < nvis ? sc[c] : 0xFF800000u;
