@@ -263,7 +263,8 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  *   first    device, [n_tokens] int32, or NULL       end      device, [n_tokens] int32, or NULL
  * The device arrays are read in stream order and may be changed behind the call.  Everything else - rows appended whatever the ranges
  * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend, on every storage.  Not under a sink +
- * window mask (KVF_ERR_UNSUPPORTED).  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
+ * window mask (KVF_ERR_UNSUPPORTED).  slopes go by row numbers, which kvf_cache_evict changes: a call with slopes is refused
+ * (KVF_ERR_UNSUPPORTED) once a token would see a row that has moved up, or one appended behind such rows.  Caps and ranges go on.  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
  * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
  * A cap rounds each score to about 2^-20 of the largest it can become.
  */
@@ -297,7 +298,7 @@ kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int
  *   mass_out   device, [n_kv_heads][out_stride] fp32: rows [0, kvf_cache_len) of each head are written, the others left alone.
  *              May be mass_in (with the same stride), must not overlap it otherwise.  Strides >= kvf_cache_len
  * Sums are fp32 and their order depends on shapes alone.  Not on quantised storage and not under a sink + window mask
- * (KVF_ERR_UNSUPPORTED).  Asynchronous on cuda_stream; uses the cache's workspace as a step does.  Under KVF_COMBINE_BEHIND it waits for
+ * (KVF_ERR_UNSUPPORTED); slopes as in a step.  Asynchronous on cuda_stream; uses the cache's workspace as a step does.  Under KVF_COMBINE_BEHIND it waits for
  * an open merge (which writes lse) as kvf_cache_flush does, and like it refuses one of another capture (KVF_ERR_INVALID_ARG).
  */
 kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int32_t appended, int64_t pos0, const kvf_scores *scores,
@@ -309,7 +310,10 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
  * first n_sink, the last n_recent, and of those between the ones with the largest mass, each KV head for itself; of equal
  * masses the lower rows stay; NaN counts as less than any number.  kvf_cache_len(to) becomes budget; `from` is not changed.
  * (The Discussion of the paper, attention-based pruning.)  Kept rows keep their rotation; the next step on `to` appends behind
- * them and takes its position from pos0, which the caller passes on (the positions do not shrink with the rows).
+ * them and takes its position from pos0, which the caller passes on (the positions do not shrink with the rows).  Where rows were
+ * left out, steps and weights with slopes are refused on `to` from then on (see kvf_scores), until it is reset, filled by another
+ * eviction, or taken back by kvf_cache_set_len to no more than the first rows that kept their places (n_sink, or fewer if they had
+ * moved before).  kvf_cache_set_len to a larger length (restored storage) is the caller's word for where its rows stand.
  *   from, to    two caches of the same heads, head_dim, dtype and storage (bf16, fp32, int8, int4), contiguous or paged in any
  *               combination, of which no byte is shared; paged caches of one pool with different pages
  *   mass        device, [n_kv_heads][mass_stride] fp32, mass_stride >= kvf_cache_len(from)

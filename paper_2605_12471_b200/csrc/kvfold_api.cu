@@ -111,6 +111,7 @@ struct kvf_cache {
     size_t plane_bytes;
     Layout lay;
     int64_t len;
+    int64_t own_rows = INT64_MAX;          // rows below this one stand where they were appended; those behind an eviction moved up
     int G;                   // query heads per KV head
     int Gp;                  // rows a token takes in the tcgen05 kernels' row layout: G rounded up to a power of two
     float scale_log2;
@@ -869,7 +870,8 @@ kvf_status on_device(const kvf_cache *c) {
     return dev == c->device ? KVF_OK : KVF_ERR_INVALID_ARG;
 }
 
-kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
+// `rows`: how many rows a call's tokens can see.
+kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc, int64_t rows) {
     if (const kvf_status s = on_device(c)) return s;
     if (!sc || !(sc->softcap >= 0.0)) return KVF_ERR_INVALID_ARG;
     if (sc->softcap > 0.0) {                 // the cap, and scores as parts of it, are fp32
@@ -880,6 +882,7 @@ kvf_status check_scores(const kvf_cache *c, const kvf_scores *sc) {
         (sc->end && check_f32(reinterpret_cast<const float *>(sc->end))))
         return KVF_ERR_INVALID_ARG;
     if (c->window > 0) return KVF_ERR_UNSUPPORTED;
+    if (sc->slopes && rows > c->own_rows) return KVF_ERR_UNSUPPORTED;          // (a row's number is no longer its position)
     return KVF_OK;
 }
 
@@ -1060,7 +1063,7 @@ kvf_status kvf_fold_step_scored(kvf_cache *c, const void *q, const void *k_new, 
                                 const kvf_scores *scores, void *out, float *lse, void *cuda_stream) {
     kvf_status s = check_step(c, n_tokens, pos0);
     if (s != KVF_OK) return s;
-    s = check_scores(c, scores);
+    s = check_scores(c, scores, c->len + n_tokens);
     if (s != KVF_OK) return s;
     if (check_ptr(q) || check_ptr(k_new) || check_ptr(v_new) || check_ptr(out)) return KVF_ERR_INVALID_ARG;
     if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return KVF_ERR_INVALID_ARG;
@@ -1072,7 +1075,7 @@ kvf_status kvf_attend_scored(kvf_cache *c, const void *q, int32_t n_tokens, int6
     if (!c) return KVF_ERR_INVALID_ARG;
     if (n_tokens < 1 || n_tokens > c->cfg.max_chunk || pos0 < 0) return KVF_ERR_INVALID_ARG;
     if (c->len < 1) return KVF_ERR_INVALID_ARG;
-    kvf_status s = check_scores(c, scores);
+    kvf_status s = check_scores(c, scores, c->len);
     if (s != KVF_OK) return s;
     if (check_ptr(q) || check_ptr(out)) return KVF_ERR_INVALID_ARG;
     if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return KVF_ERR_INVALID_ARG;
@@ -1111,7 +1114,7 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     if (c->quant || c->window > 0) return KVF_ERR_UNSUPPORTED;
     if (const kvf_status s = on_device(c)) return s;
     if (scores) {
-        const kvf_status s = check_scores(c, scores);
+        const kvf_status s = check_scores(c, scores, c->len);
         if (s != KVF_OK) return s;
     }
     if (check_ptr(q_rot) || check_f32(lse) || check_f32(mass_out) || (mass_in && check_f32(mass_in))) return KVF_ERR_INVALID_ARG;
@@ -1206,6 +1209,7 @@ kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *ma
     if (e != cudaSuccess) return cuda_fail(e, "evict launch");
     to->launches += 2;
     to->len = budget;
+    to->own_rows = budget < from->len ? std::min(from->own_rows, n_sink) : from->own_rows;
     return KVF_OK;
 }
 
@@ -1367,6 +1371,7 @@ int64_t kvf_cache_len(const kvf_cache *c) { return c ? c->len : -1; }
 kvf_status kvf_cache_reset(kvf_cache *c) {
     if (!c) return KVF_ERR_INVALID_ARG;
     c->len = 0;
+    c->own_rows = INT64_MAX;
     return KVF_OK;
 }
 
@@ -1374,6 +1379,7 @@ kvf_status kvf_cache_set_len(kvf_cache *c, int64_t len) {
     if (!c) return KVF_ERR_INVALID_ARG;
     if (len < 0 || len > c->cfg.capacity) return KVF_ERR_CAPACITY;
     c->len = len;
+    if (len <= c->own_rows) c->own_rows = INT64_MAX;       // (what moved up is forgotten)
     return KVF_OK;
 }
 
@@ -1592,7 +1598,10 @@ kvf_status batch_step(kvf_batch *b, const void *q, const void *k_new, const void
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const kvf_config &f = c0->cfg;
     const int B = (int)b->caches.size();
-    if (scores && (s = check_scores(c0, scores)) != KVF_OK) return s;
+    for (int i = 0; i < B && scores; ++i) {
+        const int own = ns ? ns[i] : n;
+        if (own > 0 && (s = check_scores(b->caches[i], scores, b->caches[i]->len + own)) != KVF_OK) return s;
+    }
     const Plan plan = make_plan(c0, n, P, B, b->part_rows, true, ragged, scores != nullptr);
     int64_t *dev_prefixes = reinterpret_cast<int64_t *>(b->workspace + b->off_lens);
     int64_t *dev_pos0s = dev_prefixes + B;
