@@ -319,7 +319,8 @@ class Cache:
 
     def rotate(self, q: torch.Tensor, pos0: Optional[int] = None, out: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """kvf_rotate_queries: the chunk's queries as a step at pos0 rotates them (default: the chunk just appended)."""
+        """kvf_rotate_queries: the chunk's queries as a step at pos0 rotates them.  Default: the last n rows' numbers, which are the positions
+        of the chunk just appended unless an eviction or a pos0 of the caller's own has parted the two."""
         n = q.shape[0]
         assert q.is_cuda and q.is_contiguous() and q.dtype == self.torch_dtype
         if out is None:
@@ -356,7 +357,8 @@ class Cache:
     def evict(self, into: "Cache", mass: torch.Tensor, budget: int, n_sink: int = 0, n_recent: int = 0,
               mass_out: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """kvf_cache_evict: `budget` rows of every KV head become the rows of `into`; returns their numbers [Hkv, budget]."""
+        """kvf_cache_evict: `budget` rows of every KV head become the rows of `into`; returns their numbers [Hkv, budget].  Positions
+        go on: from here on pass `into`'s steps (and rotate) their pos0, its default is the number of rows."""
         hkv = self.cfg.n_kv_heads
         if kept is None:
             kept = torch.empty((hkv, budget), dtype=torch.int32, device=mass.device)
