@@ -615,7 +615,8 @@ cudaError_t launch_simt_t(const MassArgs &a, cudaStream_t s) {
 
 int mass_tile_tokens(int G) { return kTile / G; }
 
-cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CUtensorMap &map_k, cudaStream_t s) {
+cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CUtensorMap &map_k, cudaStream_t s, int *launched) {
+    *launched = 0;
     MassWork w;
     w.toks = mass_tile_tokens(a.G);
     w.nkt = (int)((a.rows + kTile - 1) / kTile);
@@ -639,13 +640,20 @@ cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CU
     if (e != cudaSuccess) return e;
     const int64_t ctas = w.items < a.sms ? w.items : a.sms;
     e = launch_pdl(kernel, dim3((unsigned)ctas), dim3(kTcThreads), kMassSmem, s, a, w, ncols, map_q, map_k);
-    if (e != cudaSuccess || w.splits == 1) return e;
-    return launch_pdl(mass_sum_kernel, dim3((unsigned)((a.rows + 255) / 256), a.Hkv), dim3(256), 0, s, a, w.splits);
+    if (e != cudaSuccess) return e;
+    *launched = 1;
+    if (w.splits == 1) return e;
+    e = launch_pdl(mass_sum_kernel, dim3((unsigned)((a.rows + 255) / 256), a.Hkv), dim3(256), 0, s, a, w.splits);
+    if (e == cudaSuccess) *launched = 2;
+    return e;
 }
 
-cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s) {
-    if (dtype == 0) return a.d == 128 ? launch_simt_t<__nv_bfloat16, 128>(a, s) : launch_simt_t<__nv_bfloat16, 64>(a, s);
-    return a.d == 128 ? launch_simt_t<float, 128>(a, s) : launch_simt_t<float, 64>(a, s);
+cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s, int *launched) {
+    cudaError_t e;
+    if (dtype == 0) e = a.d == 128 ? launch_simt_t<__nv_bfloat16, 128>(a, s) : launch_simt_t<__nv_bfloat16, 64>(a, s);
+    else e = a.d == 128 ? launch_simt_t<float, 128>(a, s) : launch_simt_t<float, 64>(a, s);
+    *launched = e == cudaSuccess;
+    return e;
 }
 
 }  // namespace kvf

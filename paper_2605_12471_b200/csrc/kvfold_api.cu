@@ -1155,6 +1155,7 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
     a.parts_cap = c->part_rows_cap * f.head_dim;
     const PdlScope pdl(dependent_launches());
     cudaError_t e;
+    int launched = 0;
     if (c->tc) {
         EncodeTiledFn fn = nullptr;
         kvf_status s = encode_fn(&fn);
@@ -1164,12 +1165,12 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
         s = make_map(fn, &map_q, const_cast<void *>(q_rot), (uint64_t)f.n_q_heads, (uint64_t)n_tokens, row, row * f.n_q_heads, f.head_dim,
                      (uint32_t)c->G, (uint32_t)mass_tile_tokens(c->G));
         if (s != KVF_OK) return s;
-        e = launch_mass_tc(a, map_q, c->maps.k, static_cast<cudaStream_t>(cuda_stream));
+        e = launch_mass_tc(a, map_q, c->maps.k, static_cast<cudaStream_t>(cuda_stream), &launched);
     } else {
-        e = launch_mass_simt(a, f.dtype, static_cast<cudaStream_t>(cuda_stream));
+        e = launch_mass_simt(a, f.dtype, static_cast<cudaStream_t>(cuda_stream), &launched);
     }
+    c->launches += launched;
     if (e != cudaSuccess) return cuda_fail(e, "mass launch");
-    c->launches++;
     return KVF_OK;
 }
 

@@ -327,9 +327,10 @@ struct MassArgs {
     float *parts;                    // sums of the splits, [splits][Hkv][rows]: room for parts_cap floats
     int64_t parts_cap;
 };
-cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s);
+// (`launched`: kernels that went out)
+cudaError_t launch_mass_simt(const MassArgs &a, int dtype, cudaStream_t s, int *launched);
 int mass_tile_tokens(int G);         // tokens of a query tile: the box of map_q, over q_rot, is (64, G, that)
-cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CUtensorMap &map_k, cudaStream_t s);
+cudaError_t launch_mass_tc(const MassArgs &a, const CUtensorMap &map_q, const CUtensorMap &map_k, cudaStream_t s, int *launched);
 
 // Eviction (evict.cu).  Where the rows of a cache's planes live, in bytes: contiguous planes [Hkv][capacity][row bytes] or pages of
 // 128 rows of every KV head; quantised storage has a fp32 scale per row besides.

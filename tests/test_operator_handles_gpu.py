@@ -1,0 +1,88 @@
+"""Scored steps, weights and evictions as calls: launches counted, tensors checked, views, merges left open, forms few callers use."""
+import math
+
+import pytest
+import torch
+
+from paper_2605_12471_b200 import binding
+from tests import scored
+from tests.test_scored_gpu import BASE, HEADS, check, chunk, make, slopes_of
+from tests.test_scored_storage_gpu import H, KV, held, inputs, paged
+
+pytestmark = pytest.mark.gpu
+
+
+def test_launches_of_the_weight_are_counted():
+    for heads, rows, n, kernels in (((16, 2, 128), 2900, 2900, 2), ((16, 2, 128), 2900, 1, 1), ((8, 2, 64), 300, 40, 1)):
+        cache, gen = make(heads, "bf16", 3000, 2900, prefix=rows, seed=2)
+        q = chunk(cache, gen, n)[0]
+        lse = torch.zeros((n, heads[0]), device="cuda") + 8
+        before = cache.launch_count()
+        cache.mass(q, lse)
+        assert cache.launch_count() - before == kernels, (heads, n)
+
+
+def test_weights_in_splits_behind_open_merges():
+    """Sums of splits lie where a step's partial results do: eight steps, whose merges alternate between two sets of them."""
+    n, prefix, heads = 512, 1500, (16, 2, 128)
+    got, kept = [], []
+    for flags in (0, binding.KVF_COMBINE_BEHIND):
+        cache, gen = make(heads, "bf16", 1500 + 8 * n, n, flags=flags, prefix=prefix, seed=6)
+        for t in range(8):
+            assert cache.plan(n)[3] == 3                                 # (the step leaves a merge)
+            q, k, v = chunk(cache, gen, n)
+            lse = torch.full((n, heads[0]), math.nan, device="cuda")
+            q_rot = cache.rotate(q, pos0=len(cache))
+            out = cache.fold_step(q, k, v, lse=lse)
+            count = cache.launch_count()
+            mass = cache.mass(q_rot, lse)
+            assert t > 0 or cache.launch_count() - count == 2            # (and the weight is added up in splits)
+            kept.append((out, lse))
+            got.append((out, lse, mass))
+        cache.flush()
+        torch.cuda.synchronize()
+    for a, b in zip(got[:8], got[8:]):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert all(bool(torch.isfinite(m).all()) for _, _, m in got)
+
+
+@pytest.mark.parametrize("heads,dtype", HEADS[4:])
+@pytest.mark.parametrize("n", [1, 40, 300])
+@pytest.mark.parametrize("pos0", [0, 250, 10000])
+def test_biases_on_the_cuda_cores_of_tokens_before_among_and_behind_the_rows(heads, dtype, n, pos0):
+    prefix, h = 500, heads[0]
+    for kw in (dict(slopes=slopes_of(h)), dict(slopes=-slopes_of(h) / 16, softcap=8.0), dict(slopes=slopes_of(h) * 40)):
+        cache, gen = make(heads, dtype, 900, n, prefix=prefix, seed=12)
+        q, k, v = chunk(cache, gen, n)
+        lse = torch.empty((n, h), device="cuda")
+        out = cache.fold_step(q, k, v, pos0=pos0, lse=lse, **kw)
+        check(cache, q, k, v, n, True, lse, out, pos0, **kw)
+        out = cache.attend(q, pos0=pos0, lse=lse, **kw)
+        check(cache, q, None, None, n, False, lse, out, pos0, **kw)
+
+
+@pytest.mark.parametrize("flag", [binding.KVF_CACHE_INT8, binding.KVF_CACHE_INT4])
+@pytest.mark.parametrize("is_paged", [False, True])
+@pytest.mark.parametrize("n", [1, 4, 33, 128])
+def test_queries_alone_on_quantised_rows(flag, is_paged, n):
+    rows = 901
+    for k in range(3):
+        gen = torch.Generator(device="cuda").manual_seed(3 * n + k)
+        cfg = binding.make_config(H, KV, 128, "bf16", 1024, 1024, rope_base=BASE, flags=flag)
+        cache = paged(cfg, gen, 1)[0] if is_paged else binding.Cache(cfg)
+        cache.fold_step(*inputs(gen, rows))
+        q = inputs(gen, n)[0]
+        first = torch.randint(-50, rows + 60, (n,), generator=gen, device="cuda", dtype=torch.int32)
+        end = torch.randint(-50, rows + 60, (n,), generator=gen, device="cuda", dtype=torch.int32)
+        kw = [dict(softcap=4.0), dict(first=first, end=end), dict(softcap=6.0, slopes=slopes_of(H), end=end)][k]
+        lse = torch.empty((n, H), device="cuda")
+        out = cache.attend(q, pos0=rows + 3, lse=lse, **kw)
+        assert len(cache) == rows
+        seen = scored.ranges(n, rows, rows, False, kw.get("first"), kw.get("end"))
+        want, want_lse, bound, lse_bound = scored.attend(scored.turned(q, rows + 3, BASE), held(cache, 0, n), held(cache, 1, n), seen, 1 / math.sqrt(128),
+                                                         rows + 3, kw.get("softcap", 0.0), kw.get("slopes"))
+        assert bool(((out.double() - want).abs() <= bound).all())
+        some = want_lse > -math.inf
+        assert bool((lse[~some] == -math.inf).all()) and bool((out[~some] == 0).all())
+        assert bool(((lse.double() - want_lse).abs() <= lse_bound)[some].all())
+        assert cache.status() == binding.KVF_OK
