@@ -443,16 +443,22 @@ class Cache:
         n = self.cfg.n_kv_heads * stride
         return self.storage[off:off + 4 * n].view(torch.float32).view(self.cfg.n_kv_heads, stride)[:, :self.cfg.capacity]
 
+    def _own_plane(self, kept: str, where) -> torch.Tensor:
+        # The cache keeps a view of its own; the caller gets another, to reshape in place as it likes.  (int4: a copy, made each time.)
+        if self.cfg.flags & KVF_CACHE_INT4:
+            return self._plane(where(self._h))
+        view = getattr(self, kept)
+        if view is None:
+            view = self._plane(where(self._h))
+            setattr(self, kept, view)
+        return view.detach()
+
     def k_plane(self) -> torch.Tensor:
         """[Hkv, capacity, d] view of the rotated keys (rows >= len are not content)."""
-        if self._k_view is None or self.cfg.flags & KVF_CACHE_INT4:      # (int4: a copy, made each time)
-            self._k_view = self._plane(load().kvf_cache_k_plane(self._h))
-        return self._k_view
+        return self._own_plane("_k_view", load().kvf_cache_k_plane)
 
     def v_plane(self) -> torch.Tensor:
-        if self._v_view is None or self.cfg.flags & KVF_CACHE_INT4:
-            self._v_view = self._plane(load().kvf_cache_v_plane(self._h))
-        return self._v_view
+        return self._own_plane("_v_view", load().kvf_cache_v_plane)
 
     def plan(self, n_tokens: int, prefix_len: Optional[int] = None) -> Tuple[int, int, int, int]:
         arr = (ctypes.c_int32 * 4)()

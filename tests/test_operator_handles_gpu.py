@@ -46,6 +46,25 @@ def test_weights_in_splits_behind_open_merges():
     assert all(bool(torch.isfinite(m).all()) for _, _, m in got)
 
 
+def test_plane_views_are_the_callers_own():
+    cache, _ = make((8, 2, 128), "bf16", 300, 8)
+    for plane in (cache.k_plane, cache.v_plane):
+        view = plane()
+        view.unsqueeze_(0)
+        view.transpose_(1, 2)
+        assert plane().shape == (2, 300, 128) and plane().stride() == (300 * 128, 128, 1)
+        assert plane().data_ptr() == view.data_ptr()
+
+
+def test_unpacked_codes_are_not_kept():
+    cache = binding.Cache(binding.make_config(8, 2, 128, "bf16", 1 << 16, 8, flags=binding.KVF_CACHE_INT4))
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    cache.k_plane()
+    cache.v_plane()
+    assert torch.cuda.memory_allocated() == before
+
+
 @pytest.mark.parametrize("heads,dtype", HEADS[4:])
 @pytest.mark.parametrize("n", [1, 40, 300])
 @pytest.mark.parametrize("pos0", [0, 250, 10000])
