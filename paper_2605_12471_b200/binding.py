@@ -204,14 +204,36 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
 
 
 def _scores(softcap, slopes, first, end, heads: int, n: int, device) -> Optional[kvf_scores]:
-    """kvf_scores of a step's keywords, or None where none was given (a plain step)."""
+    """kvf_scores of a step's keywords, or None where none was given (a plain step).  `device`: a torch.device, or a tensor's get_device()."""
     if not softcap and slopes is None and first is None and end is None:
         return None
+    dev = device if type(device) is int else device.index if device.type == "cuda" else -1
+    sc = kvf_scores(softcap)
     if slopes is not None:
-        assert slopes.device == device and slopes.is_contiguous() and slopes.dtype is torch.float32 and slopes.numel() == heads
-    for t in (first, end):
-        assert t is None or (t.device == device and t.is_contiguous() and t.dtype is torch.int32 and t.numel() == n)
-    return kvf_scores(softcap, *(None if t is None else t.data_ptr() for t in (slopes, first, end)))
+        assert slopes.get_device() == dev and slopes.is_contiguous() and slopes.dtype is torch.float32 and slopes.numel() == heads
+        sc.slopes = slopes.data_ptr()
+    if first is not None:
+        assert first.get_device() == dev and first.is_contiguous() and first.dtype is torch.int32 and first.numel() == n
+        sc.first = first.data_ptr()
+    if end is not None:
+        assert end.get_device() == dev and end.is_contiguous() and end.dtype is torch.int32 and end.numel() == n
+        sc.end = end.data_ptr()
+    return sc
+
+
+def _fits(cfg: kvf_config, tokens: int, dtype, out_dtype, q, k_new, v_new, out, lse) -> bool:
+    """Whether tensors are those of `tokens` tokens on a cache of this shape: what a kernel goes by, whatever it was told.  (Results may
+    have room to spare.)"""
+    own, rows, heads, dev = tokens * cfg.n_q_heads * cfg.head_dim, tokens * cfg.n_kv_heads * cfg.head_dim, tokens * cfg.n_q_heads, q.get_device()
+    if dev < 0 or q.dtype is not dtype or q.numel() != own or not q.is_contiguous():
+        return False
+    for t in (k_new, v_new):
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.numel() != rows or not t.is_contiguous()):
+            return False
+    for t, kind, n in ((out, out_dtype, own), (lse, torch.float32, heads)):
+        if t is not None and (t.get_device() != dev or t.dtype is not kind or t.numel() < n or not t.is_contiguous()):
+            return False
+    return True
 
 
 class Cache:
@@ -219,6 +241,12 @@ class Cache:
 
     _k_view: Optional[torch.Tensor] = None      # the planes' views, made when first asked for
     _v_view: Optional[torch.Tensor] = None
+    _token: Optional[Tuple[int, int, int]] = None           # numbers of a token's queries, of its keys; its query heads
+
+    def _token_sizes(self) -> Tuple[int, int, int]:
+        h, kv, d = self.cfg.n_q_heads, self.cfg.n_kv_heads, self.cfg.head_dim
+        self._token = (h * d, kv * d, h)
+        return self._token
 
     def __init__(self, cfg: kvf_config, device: str | torch.device = "cuda", workspace: torch.Tensor | None = None):
         lib = load()
@@ -279,8 +307,13 @@ class Cache:
         n = q.shape[0]
         if out is None:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
-        scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q.device)
-        if scores is not None:
+        if softcap or slopes is not None or first is not None or end is not None:
+            scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q.get_device())
+            # (devices, types and strides of the inputs as above; what _fits does at length costs a small step 2 us of 15)
+            own, rows, heads = self._token or self._token_sizes()
+            assert q.numel() == n * own and k_new.numel() == v_new.numel() == n * rows
+            assert out.dtype is self.out_dtype and out.is_cuda and out.is_contiguous() and out.numel() >= n * own
+            assert lse is None or (lse.is_cuda and lse.is_contiguous() and lse.dtype is torch.float32 and lse.numel() >= n * heads)
             rc = lib.kvf_fold_step_scored(h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), n,
                                           lib.kvf_cache_len(h) if pos0 is None else int(pos0), ctypes.byref(scores), out.data_ptr(),
                                           None if lse is None else lse.data_ptr(), _stream_ptr(stream))
@@ -306,6 +339,7 @@ class Cache:
             out = torch.empty((n, self.cfg.n_q_heads, self.cfg.head_dim), dtype=self.out_dtype, device=q.device)
         scores = _scores(softcap, slopes, first, end, self.cfg.n_q_heads, n, q.device)
         if scores is not None:
+            assert _fits(self.cfg, n, self.torch_dtype, self.out_dtype, q, None, None, out, lse)
             rc = load().kvf_attend_scored(self._h, q.data_ptr(), n, int(len(self) if pos0 is None else pos0), ctypes.byref(scores),
                                           out.data_ptr(), lse.data_ptr() if lse is not None else None, _stream_ptr(stream))
             if rc != KVF_OK:
@@ -322,10 +356,9 @@ class Cache:
         """kvf_rotate_queries: the chunk's queries as a step at pos0 rotates them.  Default: the last n rows' numbers, which are the positions
         of the chunk just appended unless an eviction or a pos0 of the caller's own has parted the two."""
         n = q.shape[0]
-        assert q.is_cuda and q.is_contiguous() and q.dtype == self.torch_dtype
         if out is None:
             out = torch.empty_like(q)
-        assert out.is_contiguous() and out.dtype == q.dtype and out.shape == q.shape
+        assert _fits(self.cfg, n, self.torch_dtype, self.torch_dtype, q, None, None, out, None)
         rc = load().kvf_rotate_queries(self._h, q.data_ptr(), n, int(len(self) - n if pos0 is None else pos0), out.data_ptr(), _stream_ptr(stream))
         if rc != KVF_OK:
             raise KvfError(rc, "kvf_rotate_queries")
@@ -338,8 +371,7 @@ class Cache:
         """kvf_cache_mass: decay * mass plus the weight that the rotated queries [n, H, d] with denominators lse [n, H] give every
         row; mass and out are [Hkv, >= len] fp32 (out may be mass; a new [Hkv, len] tensor by default)."""
         n, rows, hkv = q_rot.shape[0], len(self), self.cfg.n_kv_heads
-        assert q_rot.is_cuda and q_rot.is_contiguous() and q_rot.dtype == self.torch_dtype
-        assert lse.device == q_rot.device and lse.is_contiguous() and lse.dtype is torch.float32 and lse.numel() == n * self.cfg.n_q_heads
+        assert _fits(self.cfg, n, self.torch_dtype, self.torch_dtype, q_rot, None, None, None, lse) and lse is not None
         if out is None:
             out = torch.empty((hkv, rows), dtype=torch.float32, device=q_rot.device)
         for t in (mass, out):
@@ -443,22 +475,25 @@ class Cache:
         n = self.cfg.n_kv_heads * stride
         return self.storage[off:off + 4 * n].view(torch.float32).view(self.cfg.n_kv_heads, stride)[:, :self.cfg.capacity]
 
-    def _own_plane(self, kept: str, where) -> torch.Tensor:
-        # The cache keeps a view of its own; the caller gets another, to reshape in place as it likes.  (int4: a copy, made each time.)
-        if self.cfg.flags & KVF_CACHE_INT4:
-            return self._plane(where(self._h))
-        view = getattr(self, kept)
-        if view is None:
-            view = self._plane(where(self._h))
-            setattr(self, kept, view)
-        return view.detach()
-
+    # (The cache keeps a view of its own; the caller gets another, to reshape in place as it likes.  int4: a copy, made each time.)
     def k_plane(self) -> torch.Tensor:
         """[Hkv, capacity, d] view of the rotated keys (rows >= len are not content)."""
-        return self._own_plane("_k_view", load().kvf_cache_k_plane)
+        if self._k_view is not None:
+            return self._k_view.detach()
+        view = self._plane(load().kvf_cache_k_plane(self._h))
+        if self.cfg.flags & KVF_CACHE_INT4:
+            return view
+        self._k_view = view
+        return view.detach()
 
     def v_plane(self) -> torch.Tensor:
-        return self._own_plane("_v_view", load().kvf_cache_v_plane)
+        if self._v_view is not None:
+            return self._v_view.detach()
+        view = self._plane(load().kvf_cache_v_plane(self._h))
+        if self.cfg.flags & KVF_CACHE_INT4:
+            return view
+        self._v_view = view
+        return view.detach()
 
     def plan(self, n_tokens: int, prefix_len: Optional[int] = None) -> Tuple[int, int, int, int]:
         arr = (ctypes.c_int32 * 4)()
@@ -623,11 +658,10 @@ class Batch:
         return out
 
     def _fold_scored(self, q, k_new, v_new, n_tokens, pos0, scores, out, lse, stream) -> torch.Tensor:
-        for t in (q, k_new, v_new):
-            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16
+        od = torch.float32 if (self.cfg.flags & KVF_OUT_F32) else torch.bfloat16
         if out is None:
-            od = torch.float32 if (self.cfg.flags & KVF_OUT_F32) else torch.bfloat16
             out = torch.empty(q.shape, dtype=od, device=q.device)
+        assert _fits(self.cfg, q.shape[0] * q.shape[1], torch.bfloat16, od, q, k_new, v_new, out, lse)
         ns = None if n_tokens is None else (ctypes.c_int32 * len(self.caches))(*[int(x) for x in n_tokens])
         arr = None if pos0 is None else (ctypes.c_int64 * len(self.caches))(*[int(p) for p in pos0])
         rc = load().kvf_batch_fold_step_scored(self._h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ns, q.shape[1], arr,

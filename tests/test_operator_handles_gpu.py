@@ -65,6 +65,36 @@ def test_unpacked_codes_are_not_kept():
     assert torch.cuda.memory_allocated() == before
 
 
+def test_tensors_of_other_shapes_and_devices_are_refused_before_any_launch():
+    cache, gen = make((8, 2, 128), "bf16", 700, 64, prefix=500)
+    q, k, v = chunk(cache, gen, 20)
+    lse, wide = torch.zeros((20, 8), device="cuda"), torch.zeros((20, 8, 128), device="cuda")
+    few, short, apart = q[:, :4].contiguous(), q[..., :64].contiguous(), torch.cat([q, q], -1)[..., :128]
+    rows, count = len(cache), cache.launch_count()
+    bad = []
+    for x in (few, short, apart, q.cpu()):
+        bad += [lambda x=x: cache.rotate(x), lambda x=x: cache.mass(x, lse), lambda x=x: cache.fold_step(x, k, v, softcap=5.0), lambda x=x: cache.attend(x, softcap=5.0)]
+    bad += [lambda: cache.rotate(q, out=few), lambda: cache.rotate(q, out=torch.empty(q.shape, dtype=q.dtype)), lambda: cache.rotate(q, out=wide),
+            lambda: cache.mass(q, lse[:10]), lambda: cache.mass(q, lse.cpu()),
+            lambda: cache.fold_step(q, k[:10].contiguous(), v, softcap=5.0), lambda: cache.fold_step(q, k, v[:, :1].contiguous(), softcap=5.0),
+            lambda: cache.fold_step(q, k, v, out=few, softcap=5.0), lambda: cache.fold_step(q, k, v, out=wide, softcap=5.0),
+            lambda: cache.fold_step(q, k, v, lse=lse[:10], softcap=5.0), lambda: cache.fold_step(q, k, v, lse=lse.half(), softcap=5.0),
+            lambda: cache.attend(q, out=few, softcap=5.0), lambda: cache.attend(q, lse=lse[:10], softcap=5.0)]
+    for f in bad:
+        with pytest.raises(AssertionError):
+            f()
+    cfg = binding.make_config(H, KV, 128, "bf16", 512, 256, rope_base=BASE)
+    batch, x = binding.Batch(paged(cfg, gen, 2)), inputs(gen, 2, 5)
+    lse2 = torch.zeros((2, 5, H), device="cuda")
+    for f in (lambda: batch.fold_step(x[0][:, :, :4].contiguous(), *x[1:], softcap=5.0), lambda: batch.fold_step(x[0], x[1][:, :4].contiguous(), x[2], softcap=5.0),
+              lambda: batch.fold_step(*x, out=x[0][:, :4].contiguous(), softcap=5.0), lambda: batch.fold_step(*x, lse=lse2[:1], softcap=5.0),
+              lambda: batch.fold_step_varlen(x[0], x[1], x[2][:1], [5, 5], softcap=5.0), lambda: batch.fold_step_varlen(*x, [5, 5], lse=lse2.double(), softcap=5.0)):
+        with pytest.raises(AssertionError):
+            f()
+    torch.cuda.synchronize()
+    assert len(cache) == rows and cache.launch_count() == count and batch.launch_count() == 0
+
+
 @pytest.mark.parametrize("heads,dtype", HEADS[4:])
 @pytest.mark.parametrize("n", [1, 40, 300])
 @pytest.mark.parametrize("pos0", [0, 250, 10000])
