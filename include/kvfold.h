@@ -264,7 +264,9 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  * The device arrays are read in stream order and may be changed behind the call.  Everything else - rows appended whatever the ranges
  * say, results, workspace, errors, KVF_COMBINE_BEHIND - as for kvf_fold_step and kvf_attend, on every storage.  Not under a sink +
  * window mask (KVF_ERR_UNSUPPORTED).  slopes go by row numbers, which kvf_cache_evict changes: a call with slopes is refused
- * (KVF_ERR_UNSUPPORTED) once a token would see a row that has moved up, or one appended behind such rows.  Caps and ranges go on.  fp32 caches compute on the CUDA cores, with no limit on magnitudes.
+ * (KVF_ERR_UNSUPPORTED) once a token would see a row that has moved up, or one appended behind such rows.  Caps and ranges go on.
+ * fp32 caches compute on the CUDA cores, with no limit on magnitudes; where a plain step has one (KVF_ERR_RANGE), a scored step
+ * reports the keys and values it appends beyond it, because a later plain step computes on them.
  * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
  * A cap rounds each score to about 2^-20 of the largest it can become.
  */

@@ -697,7 +697,8 @@ kvf_status step_impl(kvf_cache *c, const void *q, const void *k_new, const void 
     ra.page_tables = nullptr;
     ra.prefixes = nullptr; ra.pos0s = nullptr; ra.ns = nullptr;
     ra.status = reinterpret_cast<int *>(c->workspace + c->lay.status);
-    ra.range_limit = c->tc32 && plan.tc ? 65504.f : 0.f;      // the fp32 tensor-core kernel computes on fp16 halves
+    ra.range_limit = c->tc32 ? 65504.f : 0.f;      // the fp32 tensor-core kernel computes on fp16 halves
+    ra.rows_only = c->tc32 && !plan.tc;
     ra.sms = c->sm_count;
     ra.table = c->table;
 
@@ -1640,7 +1641,7 @@ kvf_status batch_step(kvf_batch *b, const void *q, const void *k_new, const void
     ra.prefixes = ragged ? dev_prefixes : nullptr;
     ra.pos0s = ragged ? dev_pos0s : nullptr;
     ra.ns = ns ? dev_ns : nullptr;
-    ra.status = nullptr; ra.range_limit = 0.f;
+    ra.status = nullptr; ra.range_limit = 0.f; ra.rows_only = 0;
     ra.sms = c0->sm_count;
     ra.table = c0->table;
 

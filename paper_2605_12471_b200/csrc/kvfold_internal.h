@@ -128,9 +128,11 @@ struct RopeAppendArgs {
     // out); n above is then the longest chunk and the stride of the members' blocks in q, k_new, v_new, q_rot
     const int64_t *ns;
     // fp32 cache whose attention runs on fp16 halves of its operands: a rotated query or key or a value
-    // above range_limit in magnitude sets code 7 in *status (range_limit = 0: no check)
+    // above range_limit in magnitude sets code 7 in *status (range_limit = 0: no check).  rows_only: queries have no limit (a scored
+    // step, which computes on the CUDA cores; a later plain step reads the rows it appends all the same)
     int *status;
     float range_limit;
+    int32_t rows_only;
     int32_t sms;                     // of the device
     RopeTable table;
 };

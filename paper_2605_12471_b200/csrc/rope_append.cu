@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kThreads, kResident) rope_append_kernel(const 
                 for (int e = 0; e < VEC; ++e) amax = fmaxf(amax, fabsf(r[e]));
             }
         }
+        if (ranged && query && a.rows_only) amax = 0.f;         // (queries are a thread's first items)
     }
     if (ranged && amax > a.range_limit) atomicCAS(a.status, 0, 7);
 }
