@@ -322,7 +322,8 @@ kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int
  *   budget      n_sink + n_recent <= budget <= kvf_cache_len(from), and <= the capacity of `to` (KVF_ERR_CAPACITY)
  *   mass_out    device, [n_kv_heads][out_stride] fp32, out_stride >= budget, not over mass: the kept rows' mass; or NULL
  *   kept        device, [n_kv_heads][budget] int32: the kept rows' numbers in `from`, ascending
- * Two kernels on cuda_stream, no workspace.
+ * Two kernels on cuda_stream, no workspace.  Rows beyond 65 504 that come into an fp32 cache whose plain steps have that limit are
+ * reported by kvf_cache_status(to) (KVF_ERR_RANGE).
  */
 kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *mass, int64_t mass_stride, int64_t n_sink, int64_t n_recent,
                            int64_t budget, float *mass_out, int64_t out_stride, int32_t *kept, void *cuda_stream);

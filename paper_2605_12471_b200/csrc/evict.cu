@@ -270,6 +270,15 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
 #pragma unroll
     for (int e = 0; e < kMoveItems; ++e)
         if (row[e] >= 0) *reinterpret_cast<uint4 *>(to + a.to.offset(g, (i0 + e * kMoveThreads) >> (lg + 1))) = v[e];
+    if (a.range_limit > 0.f) {
+        bool beyond = false;
+#pragma unroll
+        for (int e = 0; e < kMoveItems; ++e)
+            if (row[e] >= 0)
+                beyond = beyond || fabsf(__uint_as_float(v[e].x)) > a.range_limit || fabsf(__uint_as_float(v[e].y)) > a.range_limit ||
+                         fabsf(__uint_as_float(v[e].z)) > a.range_limit || fabsf(__uint_as_float(v[e].w)) > a.range_limit;
+        if (beyond) atomicCAS(a.status, 0, 7);
+    }
     // value rows behind the last one, as an append leaves them
     if (i0 == threadIdx.x) {
         const int64_t rows = a.zero_end - a.budget;

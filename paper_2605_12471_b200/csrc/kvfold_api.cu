@@ -1206,6 +1206,8 @@ kvf_status kvf_cache_evict(const kvf_cache *from, kvf_cache *to, const float *ma
     a.zero_end = (budget + kKvTile - 1) / kKvTile * kKvTile;
     if (a.zero_end > y.capacity && !to->page_table) a.zero_end = y.capacity;
     a.Hkv = x.n_kv_heads;
+    a.status = reinterpret_cast<int *>(to->workspace + to->lay.status);
+    a.range_limit = to->tc32 ? 65504.f : 0.f;          // (plain steps on `to` compute on fp16 halves of its rows)
     const PdlScope pdl(dependent_launches());
     const cudaError_t e = launch_evict(a, static_cast<cudaStream_t>(cuda_stream));
     if (e != cudaSuccess) return cuda_fail(e, "evict launch");

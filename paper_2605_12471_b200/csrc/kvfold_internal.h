@@ -363,6 +363,8 @@ struct EvictArgs {
     int64_t budget, n_sink, n_recent;
     int64_t zero_end;                // value rows [budget, zero_end) of `to` are cleared
     int32_t Hkv;
+    int *status;                     // of `to`; code 7 where an fp32 row exceeds range_limit (0: no check), as in RopeAppendArgs
+    float range_limit;
 };
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s);
 

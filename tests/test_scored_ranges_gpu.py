@@ -32,3 +32,19 @@ def test_queries_of_scored_steps_have_no_limit_and_rows_none_where_plain_steps_h
     check(cache, q, k, v, n, True, lse, out, 500, softcap=20.0)
     out = cache.attend(q, pos0=500 + n, lse=lse, softcap=20.0)
     check(cache, q, None, None, n, False, lse, out, 500 + n, softcap=20.0)
+
+
+@pytest.mark.parametrize("flags", [0, binding.KVF_FORCE_SIMT])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_rows_that_an_eviction_brings_in_are_reported_where_they_matter(flags, which):
+    """From a cache without limits, or one that has told of them itself, into one whose plain steps have them."""
+    src, gen = make((8, 2, 128), "f32", 1000, 64, prefix=900, seed=3, flags=flags)
+    plane = src.k_plane() if which == "k" else src.v_plane()
+    plane[1, 700, 77] = -1e5
+    mass = torch.rand((2, 900), generator=gen, device="cuda")
+    for kept, to_flags in ((True, 0), (False, 0), (True, binding.KVF_FORCE_SIMT)):
+        mass[1, 700] = 9.0 if kept else -1.0
+        dst, _ = make((8, 2, 128), "f32", 1000, 64, flags=to_flags)
+        src.evict(dst, mass, 400, n_sink=4, n_recent=50)
+        assert dst.status() == (binding.KVF_ERR_RANGE if kept and not to_flags else binding.KVF_OK)
+        assert src.status() == binding.KVF_OK
