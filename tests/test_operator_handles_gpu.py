@@ -135,3 +135,22 @@ def test_queries_alone_on_quantised_rows(flag, is_paged, n):
         assert bool((lse[~some] == -math.inf).all()) and bool((out[~some] == 0).all())
         assert bool(((lse.double() - want_lse).abs() <= lse_bound)[some].all())
         assert cache.status() == binding.KVF_OK
+
+
+@pytest.mark.parametrize("heads,dtype", HEADS)
+@pytest.mark.parametrize("rows", [1, 5, 127, 129])
+@pytest.mark.parametrize("n", [2, 40, 300])
+def test_many_queries_alone_on_few_rows(heads, dtype, rows, n):
+    cache, gen = make(heads, dtype, 400, n, prefix=rows, seed=rows)
+    q = chunk(cache, gen, n)[0]
+    h, scale = heads[0], 1 / math.sqrt(heads[2])
+    first = torch.randint(0, rows + 1, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    for kw in (dict(softcap=3.0), dict(first=first, slopes=slopes_of(h)), dict(end=first, softcap=8.0)):
+        lse = torch.empty((n, h), device="cuda")
+        out = cache.attend(q, pos0=rows, lse=lse, **kw)
+        check(cache, q, None, None, n, False, lse, out, rows, **kw)
+        got = cache.mass(q, lse, appended=False, **kw)
+        seen = scored.ranges(n, rows, rows, False, kw.get("first"), kw.get("end"))
+        want, bound = scored.mass(q, cache.k_plane()[:, :rows], lse, seen, scale, rows, kw.get("softcap", 0.0), kw.get("slopes"),
+                                  tensor_cores=dtype == "bf16" and heads[2] == 128)
+        assert bool(((got.double() - want).abs() <= bound).all()), kw
