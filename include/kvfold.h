@@ -252,7 +252,8 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  * Scored steps: kvf_fold_step and kvf_attend for models whose scores are more than scale * (q . k).  With s that
  * product, token i of the chunk, query head h and cache row r,
  *     s <- softcap * tanh(s / softcap)              (softcap > 0)
- *     s <- s - slopes[h] * |pos0 + i - r|           (slopes given: a bias that falls with the distance; a row's position is its index)
+ *     s <- s - slopes[h] * |pos0 + i - r|           (slopes given: a bias that falls with the distance; a row's position is its index,
+ *                                                    also in a cache that holds a later stretch of a sequence)
  *     r is seen if first[i] <= r < end[i]           (either given; else first = 0 and end = the token's own row + 1, or, for
  *                                                    kvf_attend_scored, every row the cache holds)
  * so that documents packed one after the other see only themselves (first), and a prompt sees itself both ways (end).  Entries of
@@ -268,7 +269,7 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  * fp32 caches compute on the CUDA cores, with no limit on magnitudes; where a plain step has one (KVF_ERR_RANGE), a scored step
  * reports the keys and values it appends beyond it, because a later plain step computes on them.
  * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
- * A cap rounds each score to about 2^-20 of the largest it can become.
+ * A cap rounds each score to about 2^-20 of the largest it can become.  What a hidden row holds changes no bit of a result.
  */
 typedef struct kvf_scores {
     double softcap;
@@ -299,9 +300,11 @@ kvf_status kvf_rotate_queries(kvf_cache *c, const void *q, int32_t n_tokens, int
  *   mass_in    device, [n_kv_heads][in_stride] fp32, or NULL (zeros; also where decay is 0: then it is not read)
  *   mass_out   device, [n_kv_heads][out_stride] fp32: rows [0, kvf_cache_len) of each head are written, the others left alone.
  *              May be mass_in (with the same stride), must not overlap it otherwise.  Strides >= kvf_cache_len
- * Sums are fp32 and their order depends on shapes alone.  Not on quantised storage and not under a sink + window mask
- * (KVF_ERR_UNSUPPORTED); slopes as in a step.  Asynchronous on cuda_stream; uses the cache's workspace as a step does.  Under KVF_COMBINE_BEHIND it waits for
- * an open merge (which writes lse) as kvf_cache_flush does, and like it refuses one of another capture (KVF_ERR_INVALID_ARG).
+ * Sums are fp32.  The same inputs give the same bits; the order of a row's sum and the form of its exponentials go by shapes and, among
+ * the tokens of a query tile, by their ranges, biases and denominators.  Not on quantised storage and not under a sink + window mask
+ * (KVF_ERR_UNSUPPORTED); slopes as in a step.  Asynchronous on cuda_stream; uses the cache's workspace as a step does.  Under
+ * KVF_COMBINE_BEHIND it waits for an open merge (which writes lse) as kvf_cache_flush does, and like it refuses one of
+ * another capture (KVF_ERR_INVALID_ARG).
  */
 kvf_status kvf_cache_mass(kvf_cache *c, const void *q_rot, int32_t n_tokens, int32_t appended, int64_t pos0, const kvf_scores *scores,
                           const float *lse, const float *mass_in, int64_t in_stride, float decay, float *mass_out, int64_t out_stride,

@@ -8,9 +8,11 @@
 // query heads), so that a thread has one key's row of tensor memory and the sum over queries is its own: what would be a reduction
 // over lanes in the attention kernels costs nothing here.  An item is two key tiles, which stay in shared memory while the query
 // tiles come by (L2 holds them); where the chunk is one query tile that one stays and the keys stream.
-// What bounds it: shared memory (per tile of 128 x 128: the MMAs' operands 512 cycles, half a query tile coming in 128, the columns'
-// denominators 64) beside one exponential per score, 1024 cycles of the special-function unit, of which a quarter goes through the
-// multiply-add pipe.  A decoded token is bound by the K plane's bytes.
+// What a tile of 128 x 128 needs: one exponential per score, 1024 cycles of the special-function unit, of which a quarter goes through the
+// multiply-add pipe (not under a cap); shared memory (the MMAs' operands 512 cycles, half a query tile coming in 128, the columns'
+// denominators 64).  None of these is full: 2048 tokens of 28 / 4 heads on 16 K rows keep the special-function pipe busy 66 % and the
+// multiply-add pipe 50 % of the time, capped weights of 256 tokens on 31 K rows 60 % and 45 % of the cycles that an SM has work.  A
+// decoded token is bound by the K plane's bytes.
 #include <cstddef>
 #include <type_traits>
 

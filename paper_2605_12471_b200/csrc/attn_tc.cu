@@ -224,7 +224,8 @@ struct Line {
 // kMods (bf16 rows, no window): what a scored step does to its scores (ScoreMods).  kRanged: a range of rows per token, nothing else;
 // kCapped: a cap as well; kBiased: a bias, a cap, both or neither (quantised storage has only this one).  Capped and biased scores are brought to log2 units before the softmax.
 // With ranges, a row pair's key tiles are those that its tokens see between them, cut among the groups as the line of all tiles is.
-// 256 tokens of 32 / 8 heads at prefix 31 K: plain 108 us, capped 140 (scores up to half the cap), biased 143, both 184.
+// 256 tokens of 32 / 8 heads at prefix 31 K, back to back: plain 113 us; capped at 50 with scores of deviation 2 142 (none beyond the
+// small polynomial), at 20 162, at 10 with deviation 4 312; biased 145, both (at 50) 188.
 // kRanks (bf16 rows, two streams): a cluster of that many CTAs has one row tile of one KV head, each an equal share of its key
 // tiles, and writes the output: no partial results, no merge kernel.  See the end of the kernel.
 template <bool kWindow, int kQuant, bool kPair, bool kEarly, int kRanks = 0, int kMods = kPlain>
