@@ -269,7 +269,8 @@ kvf_status kvf_attend(kvf_cache *c, const void *q, int32_t n_tokens, int64_t pos
  * fp32 caches compute on the CUDA cores, with no limit on magnitudes; where a plain step has one (KVF_ERR_RANGE), a scored step
  * reports the keys and values it appends beyond it, because a later plain step computes on them.
  * Value rows must be finite, seen or not: a row hidden from a token may be multiplied by its probability of zero.
- * A cap rounds each score to about 2^-20 of the largest it can become.  What a hidden row holds changes no bit of a result.
+ * A cap rounds each score to about 2^-20 of the largest it can become.  What a row holds that no token of the step sees changes no
+ * bit of a result; under a cap, a row that other tokens of the step see can, within that rounding.
  */
 typedef struct kvf_scores {
     double softcap;

@@ -1,4 +1,4 @@
-"""Rows that a token does not see choose none of its arithmetic: whatever finite numbers they hold, the bits are the same."""
+"""Rows that no token of a warp sees choose none of its arithmetic: whatever finite numbers they hold, the bits are the same."""
 import pytest
 import torch
 
